@@ -50,7 +50,8 @@ typedef enum {
     C2R_STAGE_ROUTE = 1,
     C2R_STAGE_PERMUTE = 2,
     C2R_STAGE_EXPERT_FFN = 3,
-    C2R_STAGE_DEDUP_DISPATCH = 4 /* pass the number of devices as E */
+    C2R_STAGE_DEDUP_DISPATCH = 4, /* pass the number of devices as E */
+    C2R_STAGE_ATTENTION = 5 /* T tokens, d = head_dim, E = query heads, K = key heads, F = max_q_len (0: decode) */
 } c2r_stage;
 
 /* Library version (major*10000 + minor*100 + patch). */
@@ -70,8 +71,8 @@ int c2r_route_chunk(void);
 /*
  * Bytes of caller-provided scratch a stage needs for the given sizes (0 when it
  * needs none).  T tokens, d model width, E experts, K experts per token, F
- * expert intermediate width (only for C2R_STAGE_EXPERT_FFN), dt the activation
- * type.  Host call, no GPU work.
+ * expert intermediate width (only for C2R_STAGE_EXPERT_FFN; the other stages'
+ * readings stand at c2r_stage), dt the activation type.  Host call, no GPU work.
  */
 size_t c2r_workspace_bytes(int stage, int64_t T, int d, int E, int K, int F, c2r_dtype dt);
 
@@ -427,6 +428,90 @@ int c2r_collaboration_degree(const int32_t *C, int E, double *P, void *stream);
  */
 int c2r_distinct_devices(const int32_t *topk_idx, int64_t T, int K, int E, const int32_t *expert_device,
                          int n_maps, int n_dev, int32_t *per_token, int64_t *totals, void *stream);
+
+/*
+ * The attention that stands beside the MoE layer in the decoder blocks of the models of Sec. 4.1, for serving (forward
+ * only, as the layer): a paged key-value cache, the norms and rotation that lead into it, and attention over it for
+ * prompts and for single new tokens.
+ *
+ * c2r_kv_cache describes a cache; every field is 64 bits wide and the strides count elements:
+ *   key j of sequence b, key head h: k + page_table[b * max_pages + j / page_size] * page_stride
+ *                                      + (j % page_size) * slot_stride + h * head_stride, head_dim elements (v alike)
+ * so both [page][head][slot][element] and [page][slot][head][element] are cache layouts, and one page per sequence is a
+ * dense cache.  page_size is any number from 1 on.  kv_len[b] counts the tokens of sequence b that the cache holds, the new
+ * ones of this step included.  page_table int32[batch, max_pages] and kv_len int32[batch] live in DEVICE memory.
+ * Lengths are cut to [0, max_pages * page_size]; a page number outside [0, n_pages) (a page given back, say) is never
+ * written and reads as page 0, which matters only if a query sees a key of it.
+ * Limits (else C2R_ERR_UNSUPPORTED): head_dim 64 or 128; up to 1024 heads; batch, pages, page_size * max_pages and tokens
+ * below 2^30.  C2R_ERR_INVALID_ARG: query heads not a multiple of kv_heads, rows or strides that are not whole 16-byte
+ * pieces, strides shorter than a row.
+ */
+typedef struct {
+    int64_t n_pages, page_size, max_pages, batch, kv_heads, head_dim, dtype, page_stride, slot_stride, head_stride;
+    void *k, *v;
+    const int32_t *page_table, *kv_len;
+} c2r_kv_cache;
+
+/*
+ * Norms of queries and keys for each head and the position rotation, in one pass (the step that leads into the attention
+ * of the decoder blocks of Sec. 4.1's models).  For every token t and head, over its head_dim elements:
+ *     y = x * rsqrt(mean(x^2) + eps) * weight          (weight null: y = x)
+ *     (y_i, y_j) -> (y_i cos a - y_j sin a, y_j cos a + y_i sin a),  a = position[t] * inv_freq[i'],  i' = 0 .. rot_dim/2 - 1
+ * with (i, j) = (i', i' + rot_dim / 2), or (2 i', 2 i' + 1) if neighbours is not 0; elements from rot_dim on are not turned.
+ * 32-bit arithmetic (the angle is reduced in 64 bits), rounded once.
+ * q : [T, heads, head_dim] of dt, q_stride elements from one token to the next (heads contiguous); k alike with kv_heads, so
+ *     slices of a joint projection are taken as they are.  q_out, k_out: the same shapes; each may be its input (same stride).
+ * q_weight, k_weight : fp32[head_dim] (16-byte aligned) or NULL;  inv_freq : fp32[rot_dim / 2];  position : int32[T]
+ *     (inv_freq and position may be NULL with rot_dim == 0).  rot_dim: a multiple of 16 up to head_dim.
+ * Limits and errors: as c2r_kv_cache.
+ */
+int c2r_qk_norm_rope(const void *q, int64_t q_stride, const void *k, int64_t k_stride, c2r_dtype dt, int64_t T, int heads, int kv_heads,
+                     int head_dim, const float *q_weight, const float *k_weight, float eps, const float *inv_freq, int rot_dim,
+                     int neighbours, const int32_t *position, void *q_out, int64_t q_out_stride, void *k_out, int64_t k_out_stride,
+                     void *stream);
+
+/*
+ * c2r_qk_norm_rope whose keys go into the cache, with the values beside them (the appending step of the decoder blocks of
+ * Sec. 4.1's models), in the same pass.  The new tokens of sequence b are rows q_start[b] .. q_start[b+1] - 1 of q, k, v and
+ * take the last places of its kv_len[b]; q_start == NULL: one token per sequence (T == batch).
+ * q_start  : int32[batch + 1] in DEVICE memory, non-decreasing; rows of no sequence are left out, their q_out untouched
+ * position : int32[T], or NULL: the token's place in the cache
+ * A token whose place is below 0 (kv_len smaller than the new tokens) is rotated and not stored.
+ */
+int c2r_qk_norm_rope_append(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride, int64_t T,
+                            int heads, const float *q_weight, const float *k_weight, float eps, const float *inv_freq, int rot_dim,
+                            int neighbours, const int32_t *q_start, const int32_t *position, const c2r_kv_cache *cache, void *q_out,
+                            int64_t q_out_stride, void *stream);
+
+/*
+ * Attention of one new token per sequence over the cache (a decoding step of the decoder blocks of Sec. 4.1's models):
+ *     out[b, h] = sum_j softmax_j(scale * q[b, h] . k_j) v_j   over the keys j that the token at p = kv_len[b] - 1 sees:
+ *     0 <= j <= p and (window == 0 or j > p - window or j < sinks)
+ * key head h / (heads / kv_heads).  window: the last keys that stay visible, 0: all; sinks: first tokens that stay visible
+ * beside a window.  A sequence without a visible key (kv_len 0) gets zeros.  What is hidden has no part in the result, an
+ * infinity or a NaN there included.  Scores, softmax and sums in 32 bits (bf16: the products' weights are rounded to bf16),
+ * rounded once.  Long caches are split over the GPU and joined, with the same bits on every run.
+ * q, out     : [batch, heads, head_dim] of the cache's dtype, strides as in c2r_qk_norm_rope
+ * max_kv_len : host; the longest kv_len of the batch (0: not known).  It only steers the split: results hold for any value.
+ * ws         : c2r_workspace_bytes(C2R_STAGE_ATTENTION, batch, head_dim, heads, kv_heads, 0, dtype) bytes, 256-aligned
+ */
+int c2r_attention_decode(const void *q, int64_t q_stride, int heads, const c2r_kv_cache *cache, int64_t max_kv_len, float scale,
+                         int64_t window, int64_t sinks, void *out, int64_t out_stride, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * The same for several new tokens per sequence: whole prompts, or chunks of them behind what is cached (the prompts of
+ * Sec. 4.3 run through the decoder blocks of Sec. 4.1).  The new tokens of sequence b are rows q_start[b] ..
+ * q_start[b+1] - 1; the last one stands at p = kv_len[b] - 1, the others before it, and their own keys are in the cache
+ * already (c2r_qk_norm_rope_append).  A token at p < 0 sees nothing: zeros.
+ * T          : rows of q and out;  q_start as in c2r_qk_norm_rope_append, not NULL; rows of no sequence are untouched
+ * max_q_len  : host; at least the most new tokens of a sequence: rows past that many are untouched.  The workspace query
+ *              covers T up to batch * max_q_len
+ * ws         : c2r_workspace_bytes(C2R_STAGE_ATTENTION, T, head_dim, heads, kv_heads, max_q_len, dtype) bytes, 256-aligned
+ * Everything else as c2r_attention_decode.
+ */
+int c2r_attention_prefill(const void *q, int64_t q_stride, int64_t T, int heads, const int32_t *q_start, int64_t max_q_len,
+                          const c2r_kv_cache *cache, int64_t max_kv_len, float scale, int64_t window, int64_t sinks, void *out,
+                          int64_t out_stride, void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -17,7 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libc2r_hip.so")
 
 F32, BF16 = 0, 1
-STAGE_COACTIVATION, STAGE_ROUTE, STAGE_PERMUTE, STAGE_EXPERT_FFN, STAGE_DEDUP_DISPATCH = 0, 1, 2, 3, 4
+STAGE_COACTIVATION, STAGE_ROUTE, STAGE_PERMUTE, STAGE_EXPERT_FFN, STAGE_DEDUP_DISPATCH, STAGE_ATTENTION = 0, 1, 2, 3, 4, 5
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_LAUNCH = 0, -1, -2, -3, -4
 _ERRNAMES = {-1: "C2R_ERR_INVALID_ARG", -2: "C2R_ERR_UNSUPPORTED", -3: "C2R_ERR_WORKSPACE",
              -4: "C2R_ERR_LAUNCH"}
@@ -27,7 +27,8 @@ EXPORTS = ["c2r_version", "c2r_route_chunk", "c2r_workspace_bytes", "c2r_build_c
            "c2r_expert_ffn_gate_up", "c2r_expert_ffn_gate_up_gather", "c2r_expert_ffn_gather", "c2r_expert_ffn_down",
            "c2r_expert_ffn_gate_up_with_shared", "c2r_expert_ffn_down_with_shared", "c2r_combine", "c2r_layer_forward",
            "c2r_place_experts", "c2r_dedup_dispatch", "c2r_dedup_dispatch_filled", "c2r_combine_partial", "c2r_combine_copies",
-           "c2r_collaboration_degree", "c2r_distinct_devices"]
+           "c2r_collaboration_degree", "c2r_distinct_devices", "c2r_qk_norm_rope", "c2r_qk_norm_rope_append",
+           "c2r_attention_decode", "c2r_attention_prefill"]
 
 
 class C2RError(RuntimeError):
@@ -76,6 +77,11 @@ def lib():
         L.c2r_combine_copies.argtypes = [vp, i32, vp, i64, i64, i32, i32, vp, vp, vp]
         L.c2r_collaboration_degree.argtypes = [vp, i32, vp, vp]
         L.c2r_distinct_devices.argtypes = [vp, i64, i32, i32, vp, i32, i32, vp, vp, vp]
+        f32 = C.c_float
+        L.c2r_qk_norm_rope.argtypes = [vp, i64, vp, i64, i32, i64, i32, i32, i32, vp, vp, f32, vp, i32, i32, vp, vp, i64, vp, i64, vp]
+        L.c2r_qk_norm_rope_append.argtypes = [vp, i64, vp, i64, vp, i64, i64, i32, vp, vp, f32, vp, i32, i32, vp, vp, C.c_char_p, vp, i64, vp]
+        L.c2r_attention_decode.argtypes = [vp, i64, i32, C.c_char_p, i64, f32, i64, i64, vp, i64, vp, sz, vp]
+        L.c2r_attention_prefill.argtypes = [vp, i64, i64, i32, vp, i64, C.c_char_p, i64, f32, i64, i64, vp, i64, vp, sz, vp]
         for name in EXPORTS[3:]:
             getattr(L, name).restype = i32
         _lib = L
@@ -405,6 +411,125 @@ def distinct_devices(topk_idx, E, expert_device, n_dev, per_token=False):
     _check("c2r_distinct_devices", lib().c2r_distinct_devices(_ptr(topk_idx), T, K, E, _ptr(maps), n_maps, n_dev,
                                                             _ptr(pt), _ptr(totals), _stream()))
     return (totals, pt) if per_token else totals
+
+
+def _heads(t: torch.Tensor, heads, dim):
+    """(address, elements from one token to the next) of rows [T, heads, dim]; a slice of a joint projection will do."""
+    assert t.is_cuda and t.dim() == 3 and t.shape[1] == heads and t.shape[2] == dim, "device-resident [T, heads, head_dim] only"
+    assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == dim), "the heads of a token must be contiguous"
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * dim
+
+
+class PagedKVCache:
+    """A paged key-value cache (c2r_kv_cache): the tensors are the caller's, nothing is copied.
+
+    k, v       : [n_pages, kv_heads, page_size, head_dim], or any strided view of that shape whose last dimension is
+                 contiguous (a cache laid out [page][slot][head] comes as its transpose(1, 2)); the same strides for both
+    page_table : int32[batch, max_pages], the pages of every sequence in order
+    kv_len     : int32[batch], tokens cached per sequence, the new ones of the step included"""
+
+    _CACHE = struct.Struct("<10q4Q")   # c2r_kv_cache
+
+    def __init__(self, k, v, page_table, kv_len):
+        self.k, self.v, self.page_table, self.kv_len = k, v, page_table, kv_len
+
+    @classmethod
+    def empty(cls, n_pages, page_size, kv_heads, head_dim, batch, max_pages, dtype, device="cuda"):
+        """A cache of zeroed lengths and no pages given out (page_table holds -1)."""
+        shape = (n_pages, kv_heads, page_size, head_dim)
+        return cls(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device),
+                   torch.full((batch, max_pages), -1, dtype=torch.int32, device=device),
+                   torch.zeros((batch,), dtype=torch.int32, device=device))
+
+    @property
+    def kv_heads(self):
+        return self.k.shape[1]
+
+    @property
+    def head_dim(self):
+        return self.k.shape[3]
+
+    def _args(self):
+        k, v, pt = self.k, self.v, self.page_table
+        assert k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.stride(3) == 1
+        assert k.is_cuda and v.is_cuda and pt.dtype == torch.int32 and self.kv_len.dtype == torch.int32
+        assert pt.dim() == 2 and self.kv_len.shape == (pt.shape[0],)
+        n_pages, heads, page_size, dim = k.shape
+        ps, hs, ss, _ = k.stride()
+        return self._CACHE.pack(n_pages, page_size, pt.shape[1], pt.shape[0], heads, dim, _dt(k), ps, ss, hs,
+                                k.data_ptr(), v.data_ptr(), _addr(pt), _addr(self.kv_len))
+
+
+def _rope_weights(q_weight, k_weight, inv_freq, position, q_start, dim, T):
+    for w in (q_weight, k_weight):
+        assert w is None or (w.dtype == torch.float32 and w.shape == (dim,))
+    assert inv_freq is None or (inv_freq.dtype == torch.float32 and inv_freq.dim() == 1)
+    assert position is None or (position.dtype == torch.int32 and position.shape == (T,))
+    assert q_start is None or (q_start.dtype == torch.int32 and q_start.dim() == 1)
+    return 0 if inv_freq is None else 2 * inv_freq.numel()
+
+
+def qk_norm_rope(q, k, inv_freq, position, q_weight=None, k_weight=None, eps=1e-6, neighbours=False, out=None):
+    """Per-head RMS norm of q[T, heads, D] and k[T, kv_heads, D] (no norm without weights) and the rotation of the first
+    2 * len(inv_freq) elements by position * inv_freq.  out = (q_out, k_out), which may be (q, k).  Returns (q_out, k_out)."""
+    T, H, D = q.shape
+    Hkv = k.shape[1]
+    assert k.shape[0] == T and k.dtype == q.dtype
+    if out is None:
+        out = (torch.empty((T, H, D), dtype=q.dtype, device=q.device), torch.empty((T, Hkv, D), dtype=q.dtype, device=q.device))
+    assert out[0].dtype == q.dtype == out[1].dtype and out[0].shape[0] == T == out[1].shape[0]
+    rot = _rope_weights(q_weight, k_weight, inv_freq, position, None, D, T)
+    _check("c2r_qk_norm_rope", lib().c2r_qk_norm_rope(
+        *_heads(q, H, D), *_heads(k, Hkv, D), _dt(q), T, H, Hkv, D, _ptr(q_weight), _ptr(k_weight), eps, _ptr(inv_freq), rot,
+        bool(neighbours), _ptr(position), *_heads(out[0], H, D), *_heads(out[1], Hkv, D), _stream()))
+    return out
+
+
+def qk_norm_rope_append(q, k, v, cache, inv_freq, q_start=None, position=None, q_weight=None, k_weight=None, eps=1e-6,
+                        neighbours=False, out=None):
+    """qk_norm_rope whose keys go into the cache, v beside them.  Rows q_start[b] .. q_start[b+1]-1 are the last places of
+    sequence b's kv_len (q_start None: one token per sequence); position None: the place in the cache.  Returns q_out."""
+    T, H, D = q.shape
+    Hkv = cache.kv_heads
+    assert k.shape[0] == T == v.shape[0] and q.dtype == k.dtype == v.dtype == cache.k.dtype and D == cache.head_dim
+    assert q_start is None or q_start.numel() == cache.kv_len.numel() + 1
+    out = torch.empty((T, H, D), dtype=q.dtype, device=q.device) if out is None else out
+    assert out.dtype == q.dtype and out.shape[0] == T
+    rot = _rope_weights(q_weight, k_weight, inv_freq, position, q_start, D, T)
+    _check("c2r_qk_norm_rope_append", lib().c2r_qk_norm_rope_append(
+        *_heads(q, H, D), *_heads(k, Hkv, D), *_heads(v, Hkv, D), T, H, _ptr(q_weight), _ptr(k_weight), eps, _ptr(inv_freq), rot,
+        bool(neighbours), _ptr(q_start), _ptr(position), cache._args(), *_heads(out, H, D), _stream()))
+    return out
+
+
+def attention_decode(q, cache, scale=None, window=0, sinks=0, max_kv_len=0, ws=None, out=None):
+    """Attention of one new token per sequence, q[batch, heads, D], over the cache.  window 0: every key; with a window the
+    first `sinks` tokens stay visible too.  max_kv_len: the longest kv_len if the host knows it.  Returns [batch, heads, D]."""
+    B, H, D = q.shape
+    assert B == cache.kv_len.numel() and q.dtype == cache.k.dtype and D == cache.head_dim
+    out = torch.empty((B, H, D), dtype=q.dtype, device=q.device) if out is None else out
+    assert out.dtype == q.dtype and out.shape[0] == B
+    scale = D ** -0.5 if scale is None else scale
+    ws = _ws(workspace_bytes(STAGE_ATTENTION, B, D, H, cache.kv_heads, 0, _dt(q)), q.device, ws)
+    _check("c2r_attention_decode", lib().c2r_attention_decode(*_heads(q, H, D), H, cache._args(), max_kv_len, scale, window, sinks,
+                                                              *_heads(out, H, D), _ptr(ws), ws.numel(), _stream()))
+    return out
+
+
+def attention_prefill(q, cache, q_start, max_q_len, scale=None, window=0, sinks=0, max_kv_len=0, ws=None, out=None):
+    """Causal attention of the new tokens of every sequence (rows q_start[b] .. q_start[b+1]-1 of q[T, heads, D], at most
+    max_q_len each) over the cache, which holds their keys already.  Returns [T, heads, D]."""
+    T, H, D = q.shape
+    assert q.dtype == cache.k.dtype and D == cache.head_dim
+    assert q_start.dtype == torch.int32 and q_start.shape == (cache.kv_len.numel() + 1,)
+    out = torch.empty((T, H, D), dtype=q.dtype, device=q.device) if out is None else out
+    assert out.dtype == q.dtype and out.shape[0] == T
+    scale = D ** -0.5 if scale is None else scale
+    ws = _ws(workspace_bytes(STAGE_ATTENTION, T, D, H, cache.kv_heads, max_q_len, _dt(q)), q.device, ws)
+    _check("c2r_attention_prefill", lib().c2r_attention_prefill(
+        *_heads(q, H, D), T, H, _ptr(q_start), max_q_len, cache._args(), max_kv_len, scale, window, sinks, *_heads(out, H, D), _ptr(ws),
+        ws.numel(), _stream()))
+    return out
 
 
 class C2RLayer:

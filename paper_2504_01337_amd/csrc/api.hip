@@ -6,6 +6,7 @@ namespace c2r {
 size_t route_workspace_bytes(int64_t T, int d, int E);
 size_t permute_workspace_bytes(int64_t T, int E, int K);
 size_t dedup_workspace_bytes(int64_t T, int n_dev);
+size_t attention_workspace_bytes(int64_t T, int D, int heads, int kv_heads, int max_q_len);
 int launch_ffn_f32_pass(int pass, const float *a, const int32_t *offsets, int E_local, int64_t A_cap, int d,
                         int F, const float *b0, const float *b1, float *out, hipStream_t st);
 int launch_ffn_bf16_pass(int pass, const uint16_t *a, const int32_t *offsets, int E_local, int64_t A_cap, int d,
@@ -58,6 +59,8 @@ extern "C" size_t c2r_workspace_bytes(int stage, int64_t T, int d, int E, int K,
         }
         case C2R_STAGE_DEDUP_DISPATCH:
             return dedup_workspace_bytes(T, E);  // E: number of devices
+        case C2R_STAGE_ATTENTION:
+            return attention_workspace_bytes(T, d, E, K, F);  // d: head width, E, K: query and key heads, F: max_q_len
         default:
             return 0;
     }
