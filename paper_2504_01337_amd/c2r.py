@@ -114,6 +114,11 @@ def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _raw_stream() -> int:
+    """The current stream's handle without the Stream object around it, which costs the host more than a short call's launch."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
 def _check(fn, rc):
     if rc != OK:
         raise C2RError(fn, rc)
@@ -413,15 +418,17 @@ def distinct_devices(topk_idx, E, expert_device, n_dev, per_token=False):
     return (totals, pt) if per_token else totals
 
 
-def _heads(t: torch.Tensor, heads, dim):
+def _rows(t: torch.Tensor, T, heads, dim, dtype):
     """(address, elements from one token to the next) of rows [T, heads, dim]; a slice of a joint projection will do."""
-    assert t.is_cuda and t.dim() == 3 and t.shape[1] == heads and t.shape[2] == dim, "device-resident [T, heads, head_dim] only"
-    assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == dim), "the heads of a token must be contiguous"
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * dim
+    s = t.stride()
+    assert t.shape == (T, heads, dim) and t.dtype is dtype and t.is_cuda, "device-resident [T, heads, head_dim] of one type only"
+    assert s[2] == 1 and (heads == 1 or s[1] == dim), "the heads of a token must be contiguous"
+    return t.data_ptr(), s[0] if T > 1 else heads * dim
 
 
 class PagedKVCache:
-    """A paged key-value cache (c2r_kv_cache): the tensors are the caller's, nothing is copied.
+    """A paged key-value cache (c2r_kv_cache): the tensors are the caller's, nothing is copied.  What they hold may change
+    from call to call (pages are given out, lengths grow); other tensors are another PagedKVCache.
 
     k, v       : [n_pages, kv_heads, page_size, head_dim], or any strided view of that shape whose last dimension is
                  contiguous (a cache laid out [page][slot][head] comes as its transpose(1, 2)); the same strides for both
@@ -429,9 +436,23 @@ class PagedKVCache:
     kv_len     : int32[batch], tokens cached per sequence, the new ones of the step included"""
 
     _CACHE = struct.Struct("<10q4Q")   # c2r_kv_cache
+    __slots__ = ("k", "v", "page_table", "kv_len", "batch", "kv_heads", "head_dim", "dtype", "args")
 
     def __init__(self, k, v, page_table, kv_len):
-        self.k, self.v, self.page_table, self.kv_len = k, v, page_table, kv_len
+        assert k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.stride(3) == 1
+        assert k.is_cuda and v.is_cuda and page_table.dtype == torch.int32 and kv_len.dtype == torch.int32
+        assert page_table.dim() == 2 and kv_len.shape == (page_table.shape[0],)
+        n_pages, heads, page_size, dim = k.shape
+        ps, hs, ss, _ = k.stride()
+        put = super().__setattr__
+        for name, value in (("k", k), ("v", v), ("page_table", page_table), ("kv_len", kv_len), ("batch", kv_len.shape[0]),
+                            ("kv_heads", heads), ("head_dim", dim), ("dtype", k.dtype)):
+            put(name, value)
+        put("args", self._CACHE.pack(n_pages, page_size, page_table.shape[1], self.batch, heads, dim, _dt(k), ps, ss, hs,
+                                     k.data_ptr(), v.data_ptr(), _addr(page_table), _addr(kv_len)))
+
+    def __setattr__(self, name, value):
+        raise AttributeError("write into the cache's tensors, or make another PagedKVCache")
 
     @classmethod
     def empty(cls, n_pages, page_size, kv_heads, head_dim, batch, max_pages, dtype, device="cuda"):
@@ -441,47 +462,26 @@ class PagedKVCache:
                    torch.full((batch, max_pages), -1, dtype=torch.int32, device=device),
                    torch.zeros((batch,), dtype=torch.int32, device=device))
 
-    @property
-    def kv_heads(self):
-        return self.k.shape[1]
 
-    @property
-    def head_dim(self):
-        return self.k.shape[3]
-
-    def _args(self):
-        k, v, pt = self.k, self.v, self.page_table
-        assert k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.stride(3) == 1
-        assert k.is_cuda and v.is_cuda and pt.dtype == torch.int32 and self.kv_len.dtype == torch.int32
-        assert pt.dim() == 2 and self.kv_len.shape == (pt.shape[0],)
-        n_pages, heads, page_size, dim = k.shape
-        ps, hs, ss, _ = k.stride()
-        return self._CACHE.pack(n_pages, page_size, pt.shape[1], pt.shape[0], heads, dim, _dt(k), ps, ss, hs,
-                                k.data_ptr(), v.data_ptr(), _addr(pt), _addr(self.kv_len))
-
-
-def _rope_weights(q_weight, k_weight, inv_freq, position, q_start, dim, T):
-    for w in (q_weight, k_weight):
-        assert w is None or (w.dtype == torch.float32 and w.shape == (dim,))
-    assert inv_freq is None or (inv_freq.dtype == torch.float32 and inv_freq.dim() == 1)
-    assert position is None or (position.dtype == torch.int32 and position.shape == (T,))
-    assert q_start is None or (q_start.dtype == torch.int32 and q_start.dim() == 1)
-    return 0 if inv_freq is None else 2 * inv_freq.numel()
+def _vec(t: Optional[torch.Tensor], dtype, n):
+    """Address of a contiguous vector of n elements (any number if None), or None."""
+    if t is None:
+        return None
+    assert t.dtype is dtype and t.dim() == 1 and (n is None or t.shape[0] == n) and t.is_cuda and t.is_contiguous()
+    return t.data_ptr()
 
 
 def qk_norm_rope(q, k, inv_freq, position, q_weight=None, k_weight=None, eps=1e-6, neighbours=False, out=None):
     """Per-head RMS norm of q[T, heads, D] and k[T, kv_heads, D] (no norm without weights) and the rotation of the first
     2 * len(inv_freq) elements by position * inv_freq.  out = (q_out, k_out), which may be (q, k).  Returns (q_out, k_out)."""
     T, H, D = q.shape
-    Hkv = k.shape[1]
-    assert k.shape[0] == T and k.dtype == q.dtype
+    Hkv, dt = k.shape[1], q.dtype
     if out is None:
-        out = (torch.empty((T, H, D), dtype=q.dtype, device=q.device), torch.empty((T, Hkv, D), dtype=q.dtype, device=q.device))
-    assert out[0].dtype == q.dtype == out[1].dtype and out[0].shape[0] == T == out[1].shape[0]
-    rot = _rope_weights(q_weight, k_weight, inv_freq, position, None, D, T)
+        out = (torch.empty((T, H, D), dtype=dt, device=q.device), torch.empty((T, Hkv, D), dtype=dt, device=q.device))
     _check("c2r_qk_norm_rope", lib().c2r_qk_norm_rope(
-        *_heads(q, H, D), *_heads(k, Hkv, D), _dt(q), T, H, Hkv, D, _ptr(q_weight), _ptr(k_weight), eps, _ptr(inv_freq), rot,
-        bool(neighbours), _ptr(position), *_heads(out[0], H, D), *_heads(out[1], Hkv, D), _stream()))
+        *_rows(q, T, H, D, dt), *_rows(k, T, Hkv, D, dt), _dt(q), T, H, Hkv, D, _vec(q_weight, torch.float32, D),
+        _vec(k_weight, torch.float32, D), eps, _vec(inv_freq, torch.float32, None), 0 if inv_freq is None else 2 * inv_freq.shape[0],
+        bool(neighbours), _vec(position, torch.int32, T), *_rows(out[0], T, H, D, dt), *_rows(out[1], T, Hkv, D, dt), _raw_stream()))
     return out
 
 
@@ -490,29 +490,38 @@ def qk_norm_rope_append(q, k, v, cache, inv_freq, q_start=None, position=None, q
     """qk_norm_rope whose keys go into the cache, v beside them.  Rows q_start[b] .. q_start[b+1]-1 are the last places of
     sequence b's kv_len (q_start None: one token per sequence); position None: the place in the cache.  Returns q_out."""
     T, H, D = q.shape
-    Hkv = cache.kv_heads
-    assert k.shape[0] == T == v.shape[0] and q.dtype == k.dtype == v.dtype == cache.k.dtype and D == cache.head_dim
-    assert q_start is None or q_start.numel() == cache.kv_len.numel() + 1
-    out = torch.empty((T, H, D), dtype=q.dtype, device=q.device) if out is None else out
-    assert out.dtype == q.dtype and out.shape[0] == T
-    rot = _rope_weights(q_weight, k_weight, inv_freq, position, q_start, D, T)
+    Hkv, dt = cache.kv_heads, cache.dtype
+    assert D == cache.head_dim
+    out = torch.empty((T, H, D), dtype=dt, device=q.device) if out is None else out
     _check("c2r_qk_norm_rope_append", lib().c2r_qk_norm_rope_append(
-        *_heads(q, H, D), *_heads(k, Hkv, D), *_heads(v, Hkv, D), T, H, _ptr(q_weight), _ptr(k_weight), eps, _ptr(inv_freq), rot,
-        bool(neighbours), _ptr(q_start), _ptr(position), cache._args(), *_heads(out, H, D), _stream()))
+        *_rows(q, T, H, D, dt), *_rows(k, T, Hkv, D, dt), *_rows(v, T, Hkv, D, dt), T, H, _vec(q_weight, torch.float32, D),
+        _vec(k_weight, torch.float32, D), eps, _vec(inv_freq, torch.float32, None), 0 if inv_freq is None else 2 * inv_freq.shape[0],
+        bool(neighbours), _vec(q_start, torch.int32, cache.batch + 1), _vec(position, torch.int32, T), cache.args,
+        *_rows(out, T, H, D, dt), _raw_stream()))
     return out
+
+
+def _attention_ws(T, H, cache, max_q_len, device, ws):
+    """(address, bytes) of a call's workspace; the tensor last, to be kept until the call is enqueued."""
+    if ws is None:
+        n = lib().c2r_workspace_bytes(STAGE_ATTENTION, T, cache.head_dim, H, cache.kv_heads, max_q_len, 0)
+        if n == 0:
+            return None, 0, None
+        ws = torch.empty(n, dtype=torch.uint8, device=device)
+    return ws.data_ptr(), ws.numel(), ws
 
 
 def attention_decode(q, cache, scale=None, window=0, sinks=0, max_kv_len=0, ws=None, out=None):
     """Attention of one new token per sequence, q[batch, heads, D], over the cache.  window 0: every key; with a window the
     first `sinks` tokens stay visible too.  max_kv_len: the longest kv_len if the host knows it.  Returns [batch, heads, D]."""
     B, H, D = q.shape
-    assert B == cache.kv_len.numel() and q.dtype == cache.k.dtype and D == cache.head_dim
-    out = torch.empty((B, H, D), dtype=q.dtype, device=q.device) if out is None else out
-    assert out.dtype == q.dtype and out.shape[0] == B
-    scale = D ** -0.5 if scale is None else scale
-    ws = _ws(workspace_bytes(STAGE_ATTENTION, B, D, H, cache.kv_heads, 0, _dt(q)), q.device, ws)
-    _check("c2r_attention_decode", lib().c2r_attention_decode(*_heads(q, H, D), H, cache._args(), max_kv_len, scale, window, sinks,
-                                                              *_heads(out, H, D), _ptr(ws), ws.numel(), _stream()))
+    dt = cache.dtype
+    assert B == cache.batch and D == cache.head_dim
+    out = torch.empty((B, H, D), dtype=dt, device=q.device) if out is None else out
+    at, n, ws = _attention_ws(B, H, cache, 0, q.device, ws)
+    _check("c2r_attention_decode", lib().c2r_attention_decode(
+        *_rows(q, B, H, D, dt), H, cache.args, max_kv_len, D ** -0.5 if scale is None else scale, window, sinks, *_rows(out, B, H, D, dt),
+        at, n, _raw_stream()))
     return out
 
 
@@ -520,15 +529,13 @@ def attention_prefill(q, cache, q_start, max_q_len, scale=None, window=0, sinks=
     """Causal attention of the new tokens of every sequence (rows q_start[b] .. q_start[b+1]-1 of q[T, heads, D], at most
     max_q_len each) over the cache, which holds their keys already.  Returns [T, heads, D]."""
     T, H, D = q.shape
-    assert q.dtype == cache.k.dtype and D == cache.head_dim
-    assert q_start.dtype == torch.int32 and q_start.shape == (cache.kv_len.numel() + 1,)
-    out = torch.empty((T, H, D), dtype=q.dtype, device=q.device) if out is None else out
-    assert out.dtype == q.dtype and out.shape[0] == T
-    scale = D ** -0.5 if scale is None else scale
-    ws = _ws(workspace_bytes(STAGE_ATTENTION, T, D, H, cache.kv_heads, max_q_len, _dt(q)), q.device, ws)
+    dt = cache.dtype
+    assert D == cache.head_dim
+    out = torch.empty((T, H, D), dtype=dt, device=q.device) if out is None else out
+    at, n, ws = _attention_ws(T, H, cache, max_q_len, q.device, ws)
     _check("c2r_attention_prefill", lib().c2r_attention_prefill(
-        *_heads(q, H, D), T, H, _ptr(q_start), max_q_len, cache._args(), max_kv_len, scale, window, sinks, *_heads(out, H, D), _ptr(ws),
-        ws.numel(), _stream()))
+        *_rows(q, T, H, D, dt), T, H, _vec(q_start, torch.int32, cache.batch + 1), max_q_len, cache.args, max_kv_len,
+        D ** -0.5 if scale is None else scale, window, sinks, *_rows(out, T, H, D, dt), at, n, _raw_stream()))
     return out
 
 
