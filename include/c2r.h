@@ -442,8 +442,8 @@ int c2r_distinct_devices(const int32_t *topk_idx, int64_t T, int K, int E, const
  * ones of this step included.  page_table int32[batch, max_pages] and kv_len int32[batch] live in DEVICE memory.
  * Lengths are cut to [0, max_pages * page_size]; a page number outside [0, n_pages) (a page given back, say) is never
  * written and reads as page 0, which matters only if a query sees a key of it.
- * Limits (else C2R_ERR_UNSUPPORTED): head_dim 64 or 128; up to 1024 heads; batch, pages, page_size * max_pages and tokens
- * below 2^30.  C2R_ERR_INVALID_ARG: query heads not a multiple of kv_heads, rows or strides that are not whole 16-byte
+ * Limits (else C2R_ERR_UNSUPPORTED): head_dim 64 or 128; up to 1024 heads; batch, pages and tokens below 2^30, page_size *
+ * max_pages below 2^28, batch * heads of a decoding step below 2^24.  C2R_ERR_INVALID_ARG: query heads not a multiple of kv_heads, rows or strides that are not whole 16-byte
  * pieces, strides shorter than a row.
  */
 typedef struct {

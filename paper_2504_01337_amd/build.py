@@ -14,7 +14,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libc2r_hip.so")
 OBJ = os.path.join(HERE, "_build")
 SOURCES = ["api.hip", "route.hip", "coact.hip", "permute.hip", "combine.hip", "ffn_f32.hip", "ffn_bf16.hip", "ffn_bf16_dma.hip", "ffn_skinny.hip", "ffn_mid.hip",
-           "dedup.hip", "metrics.hip", "attention.hip", "qk_rope.hip", "attn_stream.hip", "attn_tile.hip", "attn_join.hip"]
+           "dedup.hip", "metrics.hip", "attention.hip", "qk_rope.hip", "attn_decode.hip", "attn_rows.hip", "attn_tile.hip", "attn_join.hip"]
 # benchmark equipment (a matrix-pipe ceiling probe): its own library, loaded by bench.py only
 AID_SRC = os.path.join(HERE, "bench_aids", "probe.hip")
 AID_OUT = os.path.join(HERE, "bench_aids", "libc2r_benchaid.so")

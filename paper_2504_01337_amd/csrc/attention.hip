@@ -6,6 +6,7 @@ namespace c2r {
 
 // Row counts, lengths and positions stay below this, so that their sums and differences fit 32 bits.
 constexpr int64_t ATTN_MOST = 1ll << 30;
+constexpr int64_t ATTN_MOST_KEYS = 1ll << 28;  // of a sequence: 64 times its tiles of 16 fit, too
 constexpr int ATTN_MAX_HEADS = 1024;
 
 static int check_heads(int dt, int heads, int64_t kv_heads, int64_t D) {
@@ -28,7 +29,7 @@ static int check_cache(const c2r_kv_cache *c, int heads) {
     if (rc != C2R_OK) return rc;
     if (c->batch < 0 || c->n_pages < 1 || c->page_size < 1 || c->max_pages < 1) return C2R_ERR_INVALID_ARG;
     if (c->batch >= ATTN_MOST || c->n_pages >= ATTN_MOST || c->page_size >= ATTN_MOST || c->max_pages >= ATTN_MOST ||
-        c->page_size * c->max_pages >= ATTN_MOST)
+        c->page_size * c->max_pages >= ATTN_MOST_KEYS)
         return C2R_ERR_UNSUPPORTED;
     if (!c->page_table || !c->kv_len || !c->k || !c->v) return C2R_ERR_INVALID_ARG;
     if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->page_table, 4) || !aligned(c->kv_len, 4)) return C2R_ERR_INVALID_ARG;
@@ -74,16 +75,14 @@ static int check_rope(int dt, int heads, int64_t kv_heads, int64_t D, int64_t T,
 
 size_t attention_workspace_bytes(int64_t T, int D, int heads, int kv_heads, int max_q_len) {
     if (T <= 0 || D <= 0 || heads <= 0 || kv_heads <= 0) return 0;
-    // the most rows x parts that attn_split() gives where it gives more than one part: `blocks` blocks become at most
+    // the most rows x parts that attn_parts() gives where it gives more than one part: `blocks` blocks become at most
     // target + blocks, and each has at most per_block rows
     const int64_t rows = T * heads;
     auto bound = [rows](int64_t target, int64_t per_block) { return rows < target * per_block ? target * per_block + rows : 0; };
-    int64_t most = bound(ATTN_DECODE_BLOCKS, heads / kv_heads < 16 ? heads / kv_heads : 16);
-    if (max_q_len > 0) {
-        const int64_t tile = bound(ATTN_TILE_BLOCKS, ATTN_TILE_ROWS), full = bound(ATTN_ROWS_BLOCKS, ATTN_ROWS_ROWS);
-        most = tile > full ? tile : full;
-    }
-    return round_up((size_t)most * (size_t)(D + 2) * 4, 256);
+    if (max_q_len <= 0)
+        return round_up((size_t)bound(ATTN_DECODE_EVEN_BLOCKS, heads / kv_heads < 16 ? heads / kv_heads : 16) * (size_t)(D + 2) * 4, 256);
+    const int64_t tile = bound(ATTN_TILE_BLOCKS, ATTN_TILE_ROWS), full = bound(ATTN_ROWS_BLOCKS, ATTN_ROWS_ROWS);
+    return round_up((size_t)(tile > full ? tile : full) * (size_t)(D + 2) * 4, 256);
 }
 
 }  // namespace c2r
@@ -195,7 +194,15 @@ extern "C" int c2r_attention_decode(const void *q, int64_t q_stride, int heads, 
     if (rc != C2R_OK || cache->batch == 0) return rc;
     const bool bf16 = cache->dtype == C2R_BF16;
     const int64_t blocks = cache->batch * cache->kv_heads * ceil_div(a.group, 16);
-    attn_split(a, blocks, attn_max_tiles(a, bf16 ? 32 : 16, 1, longest(cache, max_kv_len)), ATTN_DECODE_BLOCKS, ATTN_DECODE_TILES);
+    // Few blocks: parts of 8 tiles or more (256 keys in bf16) until the GPU's 768 places are taken.  Many: long sequences in
+    // parts of 24 or more, so that a batch of ragged lengths ends evenly.  Microseconds, bf16, heads of 128:
+    //   1 x 4096 keys, 16 key heads: parts of 4, 8, 24 tiles 13.5, 13.4, 16;  1 x 32000: parts of 8, 21, 24 57, 52.5, 53
+    //   131 ragged sequences of up to 8000, 8 key heads, 1, 2, 3, 5 parts: 393, 420, 376, 371
+    //   256 ragged sequences of up to 500, 16 key heads, parts of 8 tiles and whole: 120 and 97
+    const int64_t tiles = attn_max_tiles(a, bf16 ? 32 : 16, 1, longest(cache, max_kv_len));
+    const int64_t fill = attn_parts(blocks, tiles, ATTN_DECODE_BLOCKS, ATTN_DECODE_TILES);
+    const int64_t even = attn_parts(blocks, tiles, ATTN_DECODE_EVEN_BLOCKS, ATTN_DECODE_EVEN_TILES);
+    attn_split(a, tiles, fill > even ? fill : even);
     if (blocks * a.splits >= ATTN_MOST_BLOCKS) return C2R_ERR_UNSUPPORTED;
     rc = place_parts(a, (int)cache->head_dim, ws, ws_bytes);
     return rc == C2R_OK ? launch_attn_decode(a, bf16, (int)cache->head_dim, static_cast<hipStream_t>(stream)) : rc;
@@ -218,7 +225,7 @@ extern "C" int c2r_attention_prefill(const void *q, int64_t q_stride, int64_t T,
     const int64_t blocks = cache->batch * cache->kv_heads * ceil_div((int64_t)a.max_q * a.group, per_block);
     if ((int64_t)a.max_q * a.group >= (1ll << 31)) return C2R_ERR_UNSUPPORTED;
     const int64_t tiles = attn_max_tiles(a, bf16 ? 64 : 16, ceil_div(per_block, a.group) + 1, longest(cache, max_kv_len));
-    attn_split(a, blocks, tiles, bf16 ? ATTN_TILE_BLOCKS : ATTN_ROWS_BLOCKS, bf16 ? ATTN_TILE_TILES : ATTN_ROWS_TILES);
+    attn_split(a, tiles, bf16 ? attn_parts(blocks, tiles, ATTN_TILE_BLOCKS, ATTN_TILE_TILES) : attn_parts(blocks, tiles, ATTN_ROWS_BLOCKS, ATTN_ROWS_TILES));
     if (blocks * a.splits >= ATTN_MOST_BLOCKS) return C2R_ERR_UNSUPPORTED;
     rc = place_parts(a, (int)cache->head_dim, ws, ws_bytes);
     if (rc != C2R_OK) return rc;

@@ -27,13 +27,12 @@ struct KvView {
         const int n = kv_len[b];
         return n < 0 ? 0 : (int64_t)n > most ? (int)most : n;
     }
-    // Page that holds key j of sequence b (j below length(b)); an entry outside the cache reads as page 0.
-    __device__ __forceinline__ int page(int b, int j) const {
-        const int p = table[(int64_t)b * max_pages + page_of(j)];
-        return (uint32_t)p < (uint32_t)n_pages ? p : 0;
-    }
+    // The table's entry for key j of sequence b (j below length(b)), as it stands there: nothing waits for it before it is used.
+    __device__ __forceinline__ int page(int b, int j) const { return table[(int64_t)b * max_pages + page_of(j)]; }
+    // Where key j lies; an entry outside the cache reads as page 0.
     __device__ __forceinline__ int64_t offset(int page, int j) const {
-        return page * page_bytes + (int64_t)(j - page_of(j) * page_size) * slot_bytes;
+        const int p = (uint32_t)page < (uint32_t)n_pages ? page : 0;
+        return p * page_bytes + (int64_t)(j - page_of(j) * page_size) * slot_bytes;
     }
 };
 
@@ -171,16 +170,16 @@ struct RopeCall {
 int launch_qk_norm_rope(RopeCall a, bool bf16, int D, bool neighbours, hipStream_t st);
 // attn_join.hip: out = joined partial results of a call with more than one split.
 int launch_attn_join(const AttnCall &a, bool bf16, int D, hipStream_t st);
-// attn_stream.hip: keys straight from memory to the matrix instructions, 16 rows at a time.
-//   decode: one new token per sequence, the heads of a group side by side; rows: prompts in full precision.
+// attn_decode.hip: one new token per sequence.
 int launch_attn_decode(const AttnCall &a, bool bf16, int D, hipStream_t st);
+// attn_rows.hip: prompts in full precision.
 int launch_attn_rows_f32(const AttnCall &a, int D, hipStream_t st);
 // attn_tile.hip: prompts in bf16, key tiles through LDS.
 int launch_attn_tile(const AttnCall &a, int D, hipStream_t st);
 
 // How many blocks a call is cut into at most where it has few rows, by kernel (the reasons stand beside each), and the key
 // tiles of a part.
-constexpr int ATTN_DECODE_BLOCKS = 1024, ATTN_DECODE_TILES = 4;
+constexpr int ATTN_DECODE_BLOCKS = 768, ATTN_DECODE_TILES = 8, ATTN_DECODE_EVEN_BLOCKS = 4608, ATTN_DECODE_EVEN_TILES = 24;
 constexpr int ATTN_TILE_BLOCKS = 512, ATTN_TILE_TILES = 4, ATTN_TILE_ROWS = 128;
 constexpr int ATTN_ROWS_BLOCKS = 512, ATTN_ROWS_TILES = 8, ATTN_ROWS_ROWS = 64;
 
@@ -189,12 +188,15 @@ constexpr int64_t ATTN_MOST_BLOCKS = 1ll << 24;
 
 static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Sets splits and split_tiles: `blocks` blocks without a cut, at most `tiles` key tiles each.
-static inline void attn_split(AttnCall &a, int64_t blocks, int64_t tiles, int target, int least) {
+// Parts that up to `tiles` key tiles are cut into where there are `blocks` blocks without a cut: as many as make `target`
+// blocks, of `least` tiles or more.
+static inline int64_t attn_parts(int64_t blocks, int64_t tiles, int target, int least) {
     int64_t n = ceil_div(target, blocks);
     if (n > ceil_div(tiles, least)) n = ceil_div(tiles, least);
-    if (n < 1) n = 1;
-    const int64_t each = ceil_div(tiles > 0 ? tiles : 1, n);
+    return n < 1 ? 1 : n;
+}
+static inline void attn_split(AttnCall &a, int64_t tiles, int64_t parts) {
+    const int64_t each = ceil_div(tiles > 0 ? tiles : 1, parts);
     a.split_tiles = (int)each;
     a.splits = (int)ceil_div(tiles > 0 ? tiles : 1, each);
 }

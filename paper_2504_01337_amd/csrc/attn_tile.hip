@@ -161,7 +161,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
         top = max_halves(top) * a.scale_log2;
-        // rescaled only where the maximum has grown by more than 2^8 (see attn_stream.hip)
+        // rescaled only where the maximum has grown by more than 2^8 (see attn_stream.h)
         const bool grow = top > m + 8.0f || (m == -__builtin_inff() && top > m);
         if (__any(grow)) {
             const float alpha = grow ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
