@@ -19,8 +19,11 @@ struct TileShape {
     static constexpr int RPC = 64 / CH;                  // rows per copy instruction of a wave
     static constexpr int COPIES = KT / RPC / WAVES;      // copies per wave, tile and operand
     static constexpr int BYTES = KT * D * 2;             // one operand's tile
-    // where piece c of row r is kept (D = 64: two rows span the banks, so pairs of rows share a key)
-    __device__ static __forceinline__ int place(int r, int c) { return (r * CH + (c ^ ((CH == 16 ? r : r >> 1) & (CH - 1)))) * 16; }
+    // Piece c of row r is kept at piece c ^ key(r) of it.  The keys of 256 bytes' worth of rows (16, or 8 pairs) differ, for
+    // the reads of K, which touch one piece of each; and those of four rows in a row differ in the bits that count 64 bytes,
+    // for the transposed reads of V, which touch 64 bytes of each.
+    __device__ static __forceinline__ int key(int r) { return CH == 16 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3); }
+    __device__ static __forceinline__ int place(int r, int c) { return (r * CH + (c ^ key(r))) * 16; }
 };
 
 __device__ __forceinline__ void copy16_far(const unsigned char *src, unsigned char *lds) {
@@ -36,11 +39,18 @@ __device__ __forceinline__ void copy16_far(const unsigned char *src, unsigned ch
 #endif
 }
 
-__device__ __forceinline__ u32x2 read_transposed(const unsigned char *lds) {
+// Reads at an LDS address: 16 bytes, and 4 keys of one element (see above).
+__device__ __forceinline__ bf16x8 read16(uint32_t at) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return *(const __attribute__((address_space(3))) bf16x8 *)at;
+#else
+    return bf16x8{};
+#endif
+}
+__device__ __forceinline__ u32x2 read_transposed(uint32_t at) {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef short s16x4 __attribute__((ext_vector_type(4)));
-    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)lds));
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at));
 #else
     return u32x2{};
 #endif
@@ -62,10 +72,13 @@ __device__ __forceinline__ float add_halves(float v) {
     return v;
 }
 
-template <int D>
+// ALIGNED: pages of whole groups of 16 keys, and of less than 4 GB, so that the 16 rows which a wave copies of a tile lie in
+// one page: one look-up and one scalar address.  Working out every lane's page takes as many vector instructions per tile as
+// the softmax.
+template <int D, bool ALIGNED>
 __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_blocks) {
     using T = TileShape<D>;
-    constexpr int KT = T::KT, KSTEPS = D / 16, DT = D / 32;
+    constexpr int KT = T::KT, KSTEPS = D / 16, DT = D / 32, VALU = 0x2, MFMA = 0x8, DS_READ = 0x100;
     __shared__ __align__(1024) unsigned char lds[2][2][T::BYTES];  // [buffer][K, V]
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, n = lane & 31;
     int64_t id = blockIdx.x;
@@ -96,31 +109,75 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
     int x0, x1;
     tiles.part(a, split, x0, x1);
 
-    // ---- copies: rows (wave * COPIES + u) * RPC + lane / CH of a tile; pieces in the order the LDS image wants ----
+    // ---- copies: rows first_row(u) + lane / CH of a tile; pieces in the order the LDS image wants ----
     const int64_t head_off = kv_head * a.kv.head_bytes;
-    int pages[T::COPIES];
-    auto copy_row = [&](int u) { return (wave * T::COPIES + u) * T::RPC + lane / T::CH; };
+    constexpr int WAVE_ROWS = KT / T::WAVES;
+    int pages[ALIGNED ? 1 : T::COPIES];
+    const int lane_row = lane / T::CH;
+    auto first_row = [&](int u) { return (wave * T::COPIES + u) * T::RPC; };
+    auto piece = [&](int u) { return (lane % T::CH) ^ T::key(first_row(u) + lane_row); };
+    uint32_t in_group[T::COPIES];  // ALIGNED: this lane's bytes from the wave's first row on
+    if constexpr (ALIGNED) {
+#pragma unroll
+        for (int u = 0; u < T::COPIES; ++u) in_group[u] = (u * T::RPC + lane_row) * (uint32_t)a.kv.slot_bytes + piece(u) * 16;
+    }
+    // keys past the block's last visible one stand for that one, and are masked
     auto look_up = [&](int x) {
+        const int base = tiles.base(x);
+        if constexpr (ALIGNED) {
+            pages[0] = a.kv.page(b, min(base + wave * WAVE_ROWS, bp_max));
+        } else {
 #pragma unroll
-        for (int u = 0; u < T::COPIES; ++u) pages[u] = a.kv.page(b, min(tiles.base(x) + copy_row(u), bp_max));
-    };
-    auto copy = [&](int x, int buf) {
-#pragma unroll
-        for (int u = 0; u < T::COPIES; ++u) {
-            const int r = copy_row(u), j = min(tiles.base(x) + r, bp_max);
-            const int c = (lane % T::CH) ^ ((T::CH == 16 ? r : r >> 1) & (T::CH - 1));
-            const int64_t at = a.kv.offset(pages[u], j) + head_off + c * 16;
-            copy16_far(a.kv.k + at, &lds[buf][0][(wave * T::COPIES + u) * 1024]);
-            copy16_far(a.kv.v + at, &lds[buf][1][(wave * T::COPIES + u) * 1024]);
+            for (int u = 0; u < T::COPIES; ++u) pages[u] = a.kv.page(b, min(base + first_row(u) + lane_row, bp_max));
         }
     };
+    const unsigned char *const k_head = a.kv.k + head_off, *const v_head = a.kv.v + head_off;
+    auto copy = [&](int x, int buf) {
+        const int base = tiles.base(x);
+        if constexpr (ALIGNED) {
+            const uint32_t named = __builtin_amdgcn_readfirstlane(pages[0]), page = named < (uint32_t)a.kv.n_pages ? named : 0;
+            const int j0 = min(base + wave * WAVE_ROWS, bp_max & ~(WAVE_ROWS - 1)), over = bp_max - j0;
+            const uint32_t slot = j0 - a.kv.page_of(j0) * a.kv.page_size;
+            const uint64_t at = (uint64_t)page * (uint32_t)a.kv.page_bytes + slot * (uint32_t)a.kv.slot_bytes;
+            uint32_t off[T::COPIES];
+#pragma unroll
+            for (int u = 0; u < T::COPIES; ++u) off[u] = in_group[u];
+            if (over < WAVE_ROWS - 1) {
+#pragma unroll
+                for (int u = 0; u < T::COPIES; ++u) off[u] = min(u * T::RPC + lane_row, over) * (uint32_t)a.kv.slot_bytes + piece(u) * 16;
+            }
+#pragma unroll
+            for (int u = 0; u < T::COPIES; ++u) {
+                copy16_to_lds(k_head + at, off[u], &lds[buf][0][first_row(u) * (D * 2)]);
+                copy16_to_lds(v_head + at, off[u], &lds[buf][1][first_row(u) * (D * 2)]);
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < T::COPIES; ++u) {
+                const int64_t at = a.kv.offset(pages[u], min(base + first_row(u) + lane_row, bp_max)) + piece(u) * 16;
+                copy16_far(k_head + at, &lds[buf][0][first_row(u) * (D * 2)]);
+                copy16_far(v_head + at, &lds[buf][1][first_row(u) * (D * 2)]);
+            }
+        }
+    };
+
+    // ---- reads.  Piece 2k + h of K row n lies at keys_at ^ 32k.  V rows 4h + (lane / 4) % 4 and 8 more, elements 16 of half
+    //      a piece row from 32d on: values_at ^ 64d, and ^ 32 for the row 8 further, whose key differs in that bit ----
+#if defined(__HIP_DEVICE_COMPILE__)
+    const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)&lds[0][0][0];
+#else
+    const uint32_t lds_at = 0;
+#endif
+    const uint32_t keys_at = lds_at + T::place(n, h);
+    const uint32_t values_at = lds_at + T::BYTES + T::place(h * 4 + (lane >> 2 & 3), (lane >> 4 & 1) * 2 + (lane >> 1 & 1)) + (lane & 1) * 8;
 
     f32x16 o[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
-    float m = -__builtin_inff(), l = 0.0f;
+    float m = 0.0f, l = 0.0f;  // what scores are taken against (see below); denominator over this lane's keys
+    bool bare = true;          // no score above -infinity yet
     if (x0 < x1) {
         look_up(x0);
         copy(x0, 0);
@@ -134,69 +191,153 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
             copy(x + 1, buf ^ 1);
             if (x + 2 < x1) look_up(x + 2);
         }
-        if (left <= 0 || !tile_seen<KT>(a, base, p_min, p_max)) continue;
+        // (a wave that sees nothing of a tile that others of its block see goes along: every weight comes out as zero)
+        const bool whole = tile_whole<KT>(a, base, p_min, p_max);
         f32x16 s[2];
+        bf16x8 kf[2][KSTEPS];
+        u32x4 vf[2][2][DT], w[2][2];  // V and weights of 32 keys: two products of 16 keys
+        // (the addresses are worked out where they are used: held over the loop, they would not fit the registers)
+        uint32_t ka = keys_at + buf * (2 * T::BYTES), va = values_at + buf * (2 * T::BYTES);
+        asm volatile("" : "+v"(ka), "+v"(va));
+        auto read_keys = [&](int u, int k) { kf[u][k] = read16((ka ^ (k * 32)) + u * (32 * D * 2)); };
+        auto read_values = [&](int u, int k, int d) {
+            const u32x2 lo = read_transposed((va ^ (d * 64)) + (u * 32 + k * 16) * (D * 2));
+            const u32x2 hi = read_transposed((va ^ (d * 64 + 32)) + (u * 32 + k * 16 + 8) * (D * 2));
+            vf[u][k][d] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+        };
+        // (weights stay where they are worked out, among the products beside them)
+        auto pin = [&](int u) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[u][e] = 0.0f;
-#if defined(__HIP_DEVICE_COMPILE__)
-#pragma unroll
-        for (int k = 0; k < KSTEPS; ++k)
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-                s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(lds[buf][0] + T::place(u * 32 + n, k * 2 + h)), q[k], s[u],
-                                                               0, 0, 0);
-#endif
-        if (!tile_whole<KT>(a, base, p_min, p_max)) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (!a.sees(p, base + u * 32 + (e >> 2) * 8 + h * 4 + (e & 3))) s[u][e] = -__builtin_inff();
-        }
-        float top = s[0][0];
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
-        top = max_halves(top) * a.scale_log2;
-        // rescaled only where the maximum has grown by more than 2^8 (see attn_stream.h)
-        const bool grow = top > m + 8.0f || (m == -__builtin_inff() && top > m);
-        if (__any(grow)) {
-            const float alpha = grow ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
-            if (grow) m = top;
-            l *= alpha;
-#pragma unroll
-            for (int d = 0; d < DT; ++d) o[d] *= alpha;
-        }
-        const float ref = reference_of(m);
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
+            for (int k = 0; k < 2; ++k) asm volatile("" : "+v"(w[u][k]));
+        };
+        auto mask = [&](int u) {
+            // in keys from this lane's first one on; worked out here and nowhere before (few tiles need it)
+            int first = base + u * 32;
+            asm volatile("" : "+s"(first));
+            const int at = first + h * 4, to = p - at, from = a.window ? p - a.window - at : -1, sinks = a.window ? a.sinks - at : 0;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                s[u][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], a.scale_log2, -ref));
-                l += s[u][e];
+                const int c = (e >> 2) * 8 + (e & 3);
+                if (!(c <= to && (c > from || c < sinks))) s[u][e] = -__builtin_inff();
             }
+        };
+        auto largest = [&](int u) {
+            float top = s[u][0];
+#pragma unroll
+            for (int e = 1; e < 16; ++e) top = fmaxf(top, s[u][e]);
+            return top;
+        };
+        // weights rounded to bf16 for the matrix pipe, added unrounded
+        float sums = 0.0f;
+        auto weigh = [&](int u) {
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                const float lo = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], a.scale_log2, -m));
+                const float hi = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e + 1], a.scale_log2, -m));
+                sums += lo;
+                sums += hi;
+                w[u][e >> 3][(e >> 1) & 3] = pack_bf16x2(lo, hi);
+            }
+        };
 #if defined(__HIP_DEVICE_COMPILE__)
+        auto score = [&](int u, int k) { s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u][k], q[k], s[u], 0, 0, 0); };
+        auto add = [&](int u, int k, int d) {
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[u][k][d]), __builtin_bit_cast(bf16x8, w[u][k]), o[d], 0, 0, 0);
+        };
+        // A wave issues in order, and a product holds the matrix pipe for 32 cycles: in between there is time for some eight
+        // vector instructions.  So the softmax of the first 32 keys stands among the scores of the second 32, and theirs among
+        // the first 32's values; operands are read from LDS half a stretch ahead of their products.
+        constexpr int HK = KSTEPS / 2, HV = DT;  // half of 32 keys' products
+#define STRETCH(N, READS, OTHERS)                                       \
+    _Pragma("unroll") for (int i_ = 0; i_ < (N); ++i_) {                \
+        __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);               \
+        if (READS) __builtin_amdgcn_sched_group_barrier(DS_READ, READS, 0); \
+        if (OTHERS) __builtin_amdgcn_sched_group_barrier(VALU, OTHERS, 0);  \
+    }
+        // Scores are taken against m, which starts at 0 and moves only where a row's largest score is over 2^30 away from it (or
+        // under, while nothing of the row has been added): bf16 has the exponents of fp32, so weights of 2^30 are as good as
+        // weights of 1.  It moves before anything of the tile is added, and the tile is done again: so nothing in the usual
+        // way through waits for a maximum, and the sums stay in their registers.
+        for (;;) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            // 16 keys: weights rounded to bf16 for the matrix pipe, added unrounded above
-            u32x4 w;
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) w[c] = pack_bf16x2(s[k >> 1][(k & 1) * 8 + 2 * c], s[k >> 1][(k & 1) * 8 + 2 * c + 1]);
-            const int r = k * 16 + h * 4 + ((lane >> 2) & 3), cb = ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1), off = (lane & 1) * 8;
+                for (int e = 0; e < 16; ++e) s[u][e] = 0.0f;
+            sums = 0.0f;
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                const u32x2 lo = read_transposed(lds[buf][1] + T::place(r, d * 4 + cb) + off), hi = read_transposed(lds[buf][1] + T::place(r + 8, d * 4 + cb) + off);
-                const u32x4 v = {lo[0], lo[1], hi[0], hi[1]};
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, w), o[d], 0, 0, 0);
+            for (int k = 0; k < HK; ++k) read_keys(0, k);
+#pragma unroll
+            for (int k = 0; k < KSTEPS; ++k) {
+                score(0, k);
+                if (k < HK) read_keys(0, k + HK);
+                else read_keys(1, k - HK);
             }
+            __builtin_amdgcn_sched_group_barrier(DS_READ, HK, 0);
+            STRETCH(KSTEPS, 1, 0)
+            __builtin_amdgcn_sched_barrier(0);
+            if (!whole) mask(0);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int k = 0; k < KSTEPS; ++k) {
+                score(1, k);
+                if (k < HK) read_keys(1, k + HK);
+            }
+#pragma unroll
+            for (int d = 0; d < DT; ++d) read_values(0, 0, d);
+            weigh(0);
+            float top = largest(0);
+            STRETCH(HK, 1, 64 / KSTEPS)
+            STRETCH(HK, 2 * HV / HK, 64 / KSTEPS)
+            pin(0);
+            asm volatile("" : "+v"(top));
+            __builtin_amdgcn_sched_barrier(0);
+            if (!whole) mask(1);
+            top = max_halves(fmaxf(top, largest(1))) * a.scale_log2;
+            const bool move = top > m + 30.0f || (bare && top < m - 30.0f && top != -__builtin_inff());
+            if (!__any(move)) {
+                bare = bare && top == -__builtin_inff();
+                break;
+            }
+            // by a whole number of powers of two: exact
+            const float to = __builtin_ceilf(top), alpha = !move || bare ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+            if (move) m = to;
+            l *= alpha;
+            // in place: otherwise the compiler gives the sums other registers here, and every tile pays for copies
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    float x = o[d][e];
+                    asm volatile("v_mul_f32 %0, %1, %0" : "+v"(x) : "v"(alpha));
+                    o[d][e] = x;
+                }
         }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int d = 0; d < 2 * DT; ++d) {
+            add(0, d / DT, d % DT);
+            if (d < DT) read_values(0, 1, d);
+            else read_values(1, 0, d - DT);
+        }
+        weigh(1);
+        STRETCH(2 * DT, 2, 56 / (2 * DT))
+        pin(1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int d = 0; d < 2 * DT; ++d) {
+            add(1, d / DT, d % DT);
+            if (d < DT) read_values(1, 1, d);
+        }
+        l += sums;
+        STRETCH(DT, 2, 0)
+        STRETCH(DT, 0, 0)
+#undef STRETCH
+        __builtin_amdgcn_sched_barrier(0);
 #endif
     }
     if (left <= 0) return;
     l = add_halves(l);
+    if (bare) m = -__builtin_inff();
     bool bad = not_finite(l);
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -261,8 +402,9 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
 int launch_attn_tile(const AttnCall &a, int D, hipStream_t st) {
     const int row_blocks = (int)ceil_div((int64_t)a.max_q * a.group, ATTN_TILE_ROWS);
     const dim3 grid((unsigned)((int64_t)a.splits * a.kv.kv_heads * row_blocks * a.kv.batch)), block(256);
-    if (D == 128) attn_tile_kernel<128><<<grid, block, 0, st>>>(a, row_blocks);
-    else attn_tile_kernel<64><<<grid, block, 0, st>>>(a, row_blocks);
+    const bool aligned = a.kv.page_size % 16 == 0 && a.kv.page_bytes < (1ll << 32) && a.kv.page_size * a.kv.slot_bytes < (1ll << 32);
+    if (D == 128) aligned ? attn_tile_kernel<128, true><<<grid, block, 0, st>>>(a, row_blocks) : attn_tile_kernel<128, false><<<grid, block, 0, st>>>(a, row_blocks);
+    else aligned ? attn_tile_kernel<64, true><<<grid, block, 0, st>>>(a, row_blocks) : attn_tile_kernel<64, false><<<grid, block, 0, st>>>(a, row_blocks);
     const int rc = launch_status();
     return rc == C2R_OK && a.splits > 1 ? launch_attn_join(a, true, D, st) : rc;
 }
