@@ -132,7 +132,8 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
         }
     };
     const unsigned char *const k_head = a.kv.k + head_off, *const v_head = a.kv.v + head_off;
-    auto copy = [&](int x, int buf) {
+    // copies [from, to) of a tile
+    auto copy = [&](int x, int buf, int from, int to) {
         const int base = tiles.base(x);
         if constexpr (ALIGNED) {
             const uint32_t named = __builtin_amdgcn_readfirstlane(pages[0]), page = named < (uint32_t)a.kv.n_pages ? named : 0;
@@ -147,13 +148,13 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
                 for (int u = 0; u < T::COPIES; ++u) off[u] = min(u * T::RPC + lane_row, over) * (uint32_t)a.kv.slot_bytes + piece(u) * 16;
             }
 #pragma unroll
-            for (int u = 0; u < T::COPIES; ++u) {
+            for (int u = from; u < to; ++u) {
                 copy16_to_lds(k_head + at, off[u], &lds[buf][0][first_row(u) * (D * 2)]);
                 copy16_to_lds(v_head + at, off[u], &lds[buf][1][first_row(u) * (D * 2)]);
             }
         } else {
 #pragma unroll
-            for (int u = 0; u < T::COPIES; ++u) {
+            for (int u = from; u < to; ++u) {
                 const int64_t at = a.kv.offset(pages[u], min(base + first_row(u) + lane_row, bp_max)) + piece(u) * 16;
                 copy16_far(k_head + at, &lds[buf][0][first_row(u) * (D * 2)]);
                 copy16_far(v_head + at, &lds[buf][1][first_row(u) * (D * 2)]);
@@ -177,20 +178,17 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
     float m = 0.0f, l = 0.0f;  // what scores are taken against (see below); denominator over this lane's keys
-    bool bare = true;          // no score above -infinity yet
+    bool bare = true;               // no score above -infinity yet
+    float top = -__builtin_inff();  // the last tile's largest score
     if (x0 < x1) {
         look_up(x0);
-        copy(x0, 0);
-        if (x0 + 1 < x1) look_up(x0 + 1);
+        copy(x0, 0, 0, T::COPIES);
+        look_up(x0 + 1 < x1 ? x0 + 1 : x0);
     }
     for (int x = x0; x < x1; ++x) {
         const int buf = (x - x0) & 1, base = tiles.base(x);
         wait_copies_but<0>();
         lds_barrier();
-        if (x + 1 < x1) {
-            copy(x + 1, buf ^ 1);
-            if (x + 2 < x1) look_up(x + 2);
-        }
         // (a wave that sees nothing of a tile that others of its block see goes along: every weight comes out as zero)
         const bool whole = tile_whole<KT>(a, base, p_min, p_max);
         f32x16 s[2];
@@ -218,7 +216,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int c = (e >> 2) * 8 + (e & 3);
-                if (!(c <= to && (c > from || c < sinks))) s[u][e] = -__builtin_inff();
+                s[u][e] = (c <= to) & ((c > from) | (c < sinks)) ? s[u][e] : -__builtin_inff();
             }
         };
         auto largest = [&](int u) {
@@ -228,14 +226,13 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
             return top;
         };
         // weights rounded to bf16 for the matrix pipe, added unrounded
-        float sums = 0.0f;
         auto weigh = [&](int u) {
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
                 const float lo = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], a.scale_log2, -m));
                 const float hi = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e + 1], a.scale_log2, -m));
-                sums += lo;
-                sums += hi;
+                l += lo;
+                l += hi;
                 w[u][e >> 3][(e >> 1) & 3] = pack_bf16x2(lo, hi);
             }
         };
@@ -254,64 +251,78 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
         if (READS) __builtin_amdgcn_sched_group_barrier(DS_READ, READS, 0); \
         if (OTHERS) __builtin_amdgcn_sched_group_barrier(VALU, OTHERS, 0);  \
     }
-        // Scores are taken against m, which starts at 0 and moves only where a row's largest score is over 2^30 away from it (or
-        // under, while nothing of the row has been added): bf16 has the exponents of fp32, so weights of 2^30 are as good as
-        // weights of 1.  It moves before anything of the tile is added, and the tile is done again: so nothing in the usual
-        // way through waits for a maximum, and the sums stay in their registers.
-        for (;;) {
+        // (Copies of the next tile go out in halves after the first two stretches: all at once, right behind the barrier, they
+        // wait for each other: 761 cycles of a tile's 3300.)
+        // Scores are taken against m, a whole number near the largest score of a row's first tile that has any, and moved on
+        // where a later score is over 2^30 above it: bf16 has the exponents of fp32, so weights of 2^30 are as good as weights
+        // of 1, and nothing waits for a maximum.  (A score 2^127 above the ones before it overflows, which the check of the
+        // results finds.)
+        if (__any(bare)) {
+            top = -__builtin_inff();
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < 2; ++u) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[u][e] = 0.0f;
-            sums = 0.0f;
 #pragma unroll
-            for (int k = 0; k < HK; ++k) read_keys(0, k);
-#pragma unroll
-            for (int k = 0; k < KSTEPS; ++k) {
-                score(0, k);
-                if (k < HK) read_keys(0, k + HK);
-                else read_keys(1, k - HK);
-            }
-            __builtin_amdgcn_sched_group_barrier(DS_READ, HK, 0);
-            STRETCH(KSTEPS, 1, 0)
-            __builtin_amdgcn_sched_barrier(0);
-            if (!whole) mask(0);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int k = 0; k < KSTEPS; ++k) {
-                score(1, k);
-                if (k < HK) read_keys(1, k + HK);
-            }
-#pragma unroll
-            for (int d = 0; d < DT; ++d) read_values(0, 0, d);
-            weigh(0);
-            float top = largest(0);
-            STRETCH(HK, 1, 64 / KSTEPS)
-            STRETCH(HK, 2 * HV / HK, 64 / KSTEPS)
-            pin(0);
-            asm volatile("" : "+v"(top));
-            __builtin_amdgcn_sched_barrier(0);
-            if (!whole) mask(1);
-            top = max_halves(fmaxf(top, largest(1))) * a.scale_log2;
-            const bool move = top > m + 30.0f || (bare && top < m - 30.0f && top != -__builtin_inff());
-            if (!__any(move)) {
-                bare = bare && top == -__builtin_inff();
-                break;
-            }
-            // by a whole number of powers of two: exact
-            const float to = __builtin_ceilf(top), alpha = !move || bare ? 1.0f : __builtin_amdgcn_exp2f(m - to);
-            if (move) m = to;
-            l *= alpha;
-            // in place: otherwise the compiler gives the sums other registers here, and every tile pays for copies
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    float x = o[d][e];
-                    asm volatile("v_mul_f32 %0, %1, %0" : "+v"(x) : "v"(alpha));
-                    o[d][e] = x;
+                for (int k = 0; k < KSTEPS; ++k) {
+                    read_keys(u, k);
+                    score(u, k);
                 }
+                if (!whole) mask(u);
+                top = fmaxf(top, largest(u));
+            }
+            top = max_halves(top) * a.scale_log2;
+            if (bare && top != -__builtin_inff()) m = __builtin_ceilf(top), bare = false;
+            __builtin_amdgcn_sched_barrier(0);
         }
+        float part;  // of the largest score
+        // by a whole number of powers of two: exact
+        const bool far = top > m + 30.0f;
+        if (__any(far)) {
+            const float to = __builtin_ceilf(top), alpha = far ? __builtin_amdgcn_exp2f(m - to) : 1.0f;
+            if (far) m = to;
+            l *= alpha;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] *= alpha;
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[u][e] = 0.0f;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < HK; ++k) read_keys(0, k);
+#pragma unroll
+        for (int k = 0; k < KSTEPS; ++k) {
+            score(0, k);
+            if (k < HK) read_keys(0, k + HK);
+            else read_keys(1, k - HK);
+        }
+        __builtin_amdgcn_sched_group_barrier(DS_READ, HK, 0);
+        STRETCH(KSTEPS, 1, 0)
+        __builtin_amdgcn_sched_barrier(0);
+        if (x + 1 < x1) copy(x + 1, buf ^ 1, 0, T::COPIES / 2);
+        if (!whole) mask(0);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < KSTEPS; ++k) {
+            score(1, k);
+            if (k < HK) read_keys(1, k + HK);
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) read_values(0, 0, d);
+        weigh(0);
+        part = largest(0);
+        STRETCH(HK, 1, 64 / KSTEPS)
+        STRETCH(HK, 2 * HV / HK, 64 / KSTEPS)
+        pin(0);
+        asm volatile("" : "+v"(part), "+v"(l));
+        __builtin_amdgcn_sched_barrier(0);
+        if (x + 1 < x1) {
+            copy(x + 1, buf ^ 1, T::COPIES / 2, T::COPIES);
+            look_up(x + 2 < x1 ? x + 2 : x + 1);
+        }
+        if (!whole) mask(1);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int d = 0; d < 2 * DT; ++d) {
@@ -322,15 +333,18 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
         weigh(1);
         STRETCH(2 * DT, 2, 56 / (2 * DT))
         pin(1);
+        asm volatile("" : "+v"(l));
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int d = 0; d < 2 * DT; ++d) {
             add(1, d / DT, d % DT);
             if (d < DT) read_values(1, 1, d);
         }
-        l += sums;
-        STRETCH(DT, 2, 0)
-        STRETCH(DT, 0, 0)
+        top = max_halves(fmaxf(part, largest(1))) * a.scale_log2;
+        STRETCH(DT, 2, 2)
+        STRETCH(DT, 0, 2)
+        asm volatile("" : "+v"(top));
+        __builtin_amdgcn_sched_barrier(0);
 #undef STRETCH
         __builtin_amdgcn_sched_barrier(0);
 #endif
