@@ -180,6 +180,19 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
     float m = 0.0f, l = 0.0f;  // what scores are taken against (see below); denominator over this lane's keys
     bool bare = true;               // no score above -infinity yet
     float top = -__builtin_inff();  // the last tile's largest score
+    // by a whole number of powers of two, so exact; by 2^126 at most, as 2^-127 is no normal number and would come out as zero
+    auto move = [&] {
+        const bool far = top > m + 30.0f;
+        if (!__any(far)) return;
+        const float to = fminf(__builtin_ceilf(top), m + 126.0f);
+#if defined(__HIP_DEVICE_COMPILE__)
+        const float alpha = far ? __builtin_amdgcn_exp2f(m - to) : 1.0f;
+        if (far) m = to;
+        l *= alpha;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] *= alpha;
+#endif
+    };
     if (x0 < x1) {
         look_up(x0);
         copy(x0, 0, 0, T::COPIES);
@@ -258,7 +271,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
         // of 1, and nothing waits for a maximum.  (A score 2^127 above the ones before it overflows, which the check of the
         // results finds.)
         if (__any(bare)) {
-            top = -__builtin_inff();
+            float here = -__builtin_inff();
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
 #pragma unroll
@@ -269,22 +282,14 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
                     score(u, k);
                 }
                 if (!whole) mask(u);
-                top = fmaxf(top, largest(u));
+                here = fmaxf(here, largest(u));
             }
-            top = max_halves(top) * a.scale_log2;
+            top = fmaxf(top, max_halves(here) * a.scale_log2);
             if (bare && top != -__builtin_inff()) m = __builtin_ceilf(top), bare = false;
             __builtin_amdgcn_sched_barrier(0);
         }
         float part;  // of the largest score
-        // by a whole number of powers of two: exact
-        const bool far = top > m + 30.0f;
-        if (__any(far)) {
-            const float to = __builtin_ceilf(top), alpha = far ? __builtin_amdgcn_exp2f(m - to) : 1.0f;
-            if (far) m = to;
-            l *= alpha;
-#pragma unroll
-            for (int d = 0; d < DT; ++d) o[d] *= alpha;
-        }
+        move();
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -350,6 +355,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
 #endif
     }
     if (left <= 0) return;
+    move();  // (sums of 2^100 and more would not join with those of other blocks)
     l = add_halves(l);
     if (bare) m = -__builtin_inff();
     bool bad = not_finite(l);

@@ -202,6 +202,39 @@ def test_append_to_many_sequences(c2r):
         assert torch.equal(cache.v, want), B
 
 
+@pytest.mark.parametrize("R", [128, 64])
+def test_append_of_many_tokens(c2r, R):
+    """Enough tokens that a wave takes several: sequences begin at odd rows, 70 and 130 of them in a row are empty, the first rows
+    and the last ones are of no sequence."""
+    rng = np.random.default_rng(29 + R)
+    D, H, Hkv, page, before, behind = 128, 14, 1, 64, 3, 6
+    new = [2001] + [0] * 70 + [1, 1, 1, 3001] + [0] * 130 + [2048, 5, 7301, 1]
+    lens = [n + int(rng.integers(0, 3)) for n in new]
+    lens[-4] -= 10                                  # fewer held than new: the first of them are not stored
+    bt = Batch(c2r, rng, "bf16", D, Hkv, page, lens, new, junk=3.0, spare=0)
+    T = before + bt.T + behind
+    assert T * -(-(H + 2 * Hkv) // 16) >= 8192
+    q, k, v = _randn(rng, T, H, D, dtype="bf16"), _randn(rng, T, Hkv, D, dtype="bf16"), _randn(rng, T, Hkv, D, dtype="bf16")
+    f, w = _freq(R), _randn(rng, D)
+    q_start = bt.q_start + before
+    out = torch.full((T, H, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    bt.cache.k.fill_(3.0), bt.cache.v.fill_(3.0)
+    c2r.qk_norm_rope_append(q, k, v, bt.cache, f, q_start, None, w, w, 1e-6, out=out)
+    assert (out[:before] == 7).all() and (out[T - behind:] == 7).all()
+    pos = np.concatenate([np.arange(n - m, n) for n, m in zip(lens, new)])
+    inner = slice(before, before + bt.T)
+    ok = pos >= 0
+    _check_rope(out[inner][torch.from_numpy(ok).cuda()], q[inner][torch.from_numpy(ok).cuda()], w, 1e-6, f, pos[ok], False, "bf16")
+    seq = np.repeat(np.arange(len(new)), new)
+    pages = bt.table[seq[ok], pos[ok] // page]
+    pages, slots = torch.from_numpy(pages.astype(np.int64)).cuda(), torch.from_numpy(pos[ok] % page).cuda()
+    keep = torch.from_numpy(ok).cuda()
+    _check_rope(bt.cache.k[pages, :, slots], k[inner][keep], w, 1e-6, f, pos[ok], False, "bf16")
+    assert torch.equal(bt.cache.v[pages, :, slots], v[inner][keep])
+    bt.cache.k[pages, :, slots], bt.cache.v[pages, :, slots] = 3.0, 3.0
+    assert (bt.cache.k == 3).all() and (bt.cache.v == 3).all()      # and nothing else was written
+
+
 # ---- single tokens ----
 
 LENS = [0, 1, 15, 16, 17, 31, 32, 33, 64, 129]
@@ -375,6 +408,30 @@ def test_prefill_of_large_scores(c2r, dtype):
     bt.write(0, k, v)
     q = _randn(rng, 300, 2, 64, dtype=dtype, scale=3.0)
     _check_attention(c2r.attention_prefill(q, bt.cache, bt.q_start, 300, 1.0), q, bt, dtype, 1.0, 0, 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("shape", ["rising", "saw", "spike", "falling"])
+@pytest.mark.parametrize("powers", [20, 31, 60, 140])
+def test_scores_that_jump_along_the_keys(c2r, dtype, D, shape, powers):
+    """Runs of 64 keys whose scores differ by so many powers of two; a prompt behind a context, and its last token alone."""
+    rng = np.random.default_rng(31 + D + powers)
+    new, n = 150, 900
+    bt = Batch(c2r, rng, dtype, D, 1, 16, [n], [new])
+    run = np.arange(n) // 64
+    level = {"rising": run, "saw": run * 5 % 3, "spike": (run == 9) * 1, "falling": -run}[shape] * powers * np.log(2.0)
+    k, v = bt.rows[0]
+    k *= 0.3
+    k[:, 0, 0] = torch.from_numpy(level).cuda().to(k.dtype)
+    bt.write(0, k, v)
+    q = _randn(rng, new, 2, D, dtype=dtype)
+    q[:, :, 0] = 1.0
+    _check_attention(c2r.attention_prefill(q, bt.cache, bt.q_start, new, 1.0), q, bt, dtype, 1.0, 0, 0)
+    _check_attention(c2r.attention_prefill(q, bt.cache, bt.q_start, new, 1.0, 300, 10), q, bt, dtype, 1.0, 300, 10)
+    bt.new = [1]
+    last = q[-1:].contiguous()
+    _check_attention(c2r.attention_decode(last, bt.cache, 1.0), last, bt, dtype, 1.0, 0, 0)
 
 
 # ---- both ----
