@@ -3,16 +3,25 @@
 //     y = x * rsqrt(mean(x^2) + eps) * w          (no norm without weights)
 //     the first R elements in pairs (i, j): y_i cos - y_j sin, y_j cos + y_i sin at the angle position * inv_freq[i]
 //
-// A lane holds 16 bytes of a head's row, D * size / 16 lanes a head; a wave takes several heads of ONE token in turn, so the
-// angles of its elements are worked out once.  The angle is a product in 64 bits, in turns, less its whole turns: at position
-// 100000 a 32-bit product would be off by 4e-3 radians, more than bf16 resolves.  v_sin_f32 and v_cos_f32 take turns and are
-// within 1.3e-7 of sin and cos over one turn (2^20 arguments tried).  Everything is 32 bits wide up to the one rounding.
-// Memory bound: every row read and written once.
+// A lane holds 16 bytes of a head's row, D * size / 16 lanes a head; a wave takes the heads of ONE token in turn, four groups of
+// them in flight, so the angles of its elements are worked out once a token.  The angle is a product in 64 bits, in turns, less
+// its whole turns: at position 100000 a 32-bit product would be off by 4e-3 radians, more than bf16 resolves.  v_sin_f32 and
+// v_cos_f32 take turns and are within 1.3e-7 of sin and cos over one turn (2^20 arguments tried).  Everything is 32 bits wide up
+// to the one rounding.
+// Memory bound for many tokens: every row is read and written once.  8192 tokens, 16 query and 16 key heads of 128, bf16, 201 MB
+// with the appended values: 43 us, 4.7 TB/s (a large copy runs at 4.9); without a cache, 134 MB, 26.7 us, 5.0 TB/s.  Few tokens: a
+// chain of loads (sequence, length, page) behind a launch, 4.5 us for 1 to 64 tokens.
 #include <type_traits>
 
 #include "attn_common.h"
 
 namespace c2r {
+
+// Waves of one token and of ROPE_TOKENS tokens: a launch that would have ROPE_MANY waves or more at a token each, all heads of
+// the token in one wave (four groups of heads), takes the second.  us with one, two and four tokens a wave (bf16, D 128): 8192
+// tokens of 16/16 heads 49.2, 43.0, 44.2, without a cache 30.6, 26.7, 28.2; 16000 of 32/4 heads 80.6, 69.2, 67.5; 4096 of 32/32
+// 37.8, 40.1, 56.5; pairs of neighbours 31.0, 29.5, 36.6.  Below: 2000 tokens of 16/16 19.0 and 19.8, 2005 of 32/8 18.6 and 20.1.
+constexpr int ROPE_TOKENS = 2, ROPE_MANY = 8192;
 
 // The sequence that row t belongs to, or -1 past the last one: how many of q_start[0 .. batch] are at most t, 64 at a time.
 __device__ __forceinline__ int sequence_of(const int32_t *q_start, int batch, int64_t t) {
@@ -47,18 +56,28 @@ __device__ __forceinline__ float head_sum(float v) {
     return v;
 }
 
-template <bool BF16, int D, bool CACHE, bool NEIGHBOURS>
+// TOKENS: tokens in a row that a wave takes.  Their places are looked up side by side, a lane each: the chain of loads behind a
+// place (sequence, length, page) is what a wave that is only just long enough for one token spends its life on.
+// PAIRS: where the two elements of a pair stand in the lanes.  NEAR (neighbours): one lane.  FAR (halves, the whole head turned):
+// one lane too, which then holds 8 bytes of each half.  PART (halves of a part of the head): a lane has 16 bytes in a row, and
+// its partners' come by an exchange; they are normed and their angles worked out twice.  (Whole heads the PART way: 52.3 us for
+// the 8192 tokens with their append, FAR 43.0.)
+enum Pairs { NEAR, FAR, PART };
+template <bool BF16, int D, bool CACHE, Pairs PAIRS, int TOKENS>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeCall a) {
     constexpr int SZ = BF16 ? 2 : 4, EPL = 16 / SZ, LH = D / EPL, HW = 64 / LH, BATCH = 4;
     const int lane = lane_id(), sub = lane / LH, c = lane % LH, e0 = c * EPL;
+    // this lane's two 8-byte pieces of a row: bytes
+    const int low = PAIRS == FAR ? c * 8 : c * 16, high = PAIRS == FAR ? D * SZ / 2 + c * 8 : low + 8;
     const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t t = w / a.parts;
-    const int part = (int)(w - t * a.parts);
-    if (t >= a.T) return;
-    const int total = a.heads + (CACHE ? 2 : 1) * a.kv_heads;
-    // the first rows are on their way while the position is looked up
+    const int64_t run = w / a.parts, first_token = run * TOKENS;
+    const int part = (int)(w - run * a.parts);
+    if (first_token >= a.T) return;
+    const int tokens = a.T - first_token < TOKENS ? (int)(a.T - first_token) : TOKENS;
+    const int total = a.heads + (CACHE ? 2 : 1) * a.kv_heads, groups = (total + HW - 1) / HW;
     u32x4 x[BATCH] = {};
-    auto fetch = [&](int first) {
+    // the rows of head groups first, first + parts, ... of token t
+    auto fetch = [&](int64_t t, int first) {
 #pragma unroll
         for (int u = 0; u < BATCH; ++u) {
             const int h = (first + u * a.parts) * HW + sub;
@@ -66,65 +85,97 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeCall a) {
             const unsigned char *row = h < a.heads ? a.q + t * a.q_bytes + (int64_t)h * (D * SZ)
                                        : h < a.heads + a.kv_heads ? a.k + t * a.k_bytes + (int64_t)(h - a.heads) * (D * SZ)
                                                                   : a.v + t * a.v_bytes + (int64_t)(h - a.heads - a.kv_heads) * (D * SZ);
-            x[u] = *reinterpret_cast<const u32x4 *>(row + c * 16);
+            if constexpr (PAIRS == FAR) {
+                const u32x2 a0 = *reinterpret_cast<const u32x2 *>(row + low), a1 = *reinterpret_cast<const u32x2 *>(row + high);
+                x[u] = u32x4{a0[0], a0[1], a1[0], a1[1]};
+            } else {
+                x[u] = *reinterpret_cast<const u32x4 *>(row + low);
+            }
         }
     };
-    fetch(part);
-
-    int index = 0;           // place in the sequence's cache
-    int64_t cache_off = -1;  // bytes from the cache's start, -1: no such place
-    if constexpr (CACHE) {
-        const int b = a.q_start ? sequence_of(a.q_start, a.kv.batch, t) : (int)t;
-        if (b < 0) return;  // rows of no sequence
-        const int len = a.kv.length(b);
-        if (a.q_start) {
-            const int64_t end = a.q_start[b + 1];
-            index = len - (int)((end < a.T ? end : a.T) - t);
+    auto store = [&](unsigned char *row, const u32x4 &v) {
+        if constexpr (PAIRS == FAR) {
+            *reinterpret_cast<u32x2 *>(row + low) = u32x2{v[0], v[1]};
+            *reinterpret_cast<u32x2 *>(row + high) = u32x2{v[2], v[3]};
         } else {
-            index = len - 1;
-        }
-        if (index >= 0) {
-            const int page = a.kv.table[(int64_t)b * a.kv.max_pages + a.kv.page_of(index)];
-            if ((uint32_t)page < (uint32_t)a.kv.n_pages) cache_off = a.kv.offset(page, index);
-        }
-    }
-    const int pos = a.position ? a.position[t] : index;
-    // partner of this lane's elements, their angles
-    const int half = a.rot / 2, hl = half / EPL;
-    const bool turned = e0 < a.rot;
-    const int partner = NEIGHBOURS || !turned ? c : c < hl ? c + hl : c - hl;
-    constexpr int NA = NEIGHBOURS ? EPL / 2 : EPL;
-    float cs[NA], sn[NA];
-#pragma unroll
-    for (int i = 0; i < NA; ++i) {
-        cs[i] = 1.0f, sn[i] = 0.0f;
-        if (turned) {
-            const int f = NEIGHBOURS ? e0 / 2 + i : (c < hl ? e0 : e0 - half) + i;
-            const double turns = (double)pos * (double)a.inv_freq[f] * 0.15915494309189533577;
-            const float r = (float)(turns - __builtin_rint(turns));
-#if defined(__HIP_DEVICE_COMPILE__)
-            cs[i] = __builtin_amdgcn_cosf(r);
-            sn[i] = __builtin_amdgcn_sinf(r);
-#endif
-            if (!NEIGHBOURS && c < hl) sn[i] = -sn[i];  // y_i cos - y_j sin; y_j cos + y_i sin
-        }
-    }
-    // weights of this lane's elements and of their partners
-    float wq[EPL], wk[EPL], wq_other[EPL], wk_other[EPL];
-    auto weights = [&](const float *src, int at, float (&f)[EPL]) {
-#pragma unroll
-        for (int i = 0; i < EPL; i += 4) {
-            const f32x4 v = src ? *reinterpret_cast<const f32x4 *>(src + at + i) : f32x4{1.0f, 1.0f, 1.0f, 1.0f};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) f[i + j] = v[j];
+            *reinterpret_cast<u32x4 *>(row + low) = v;
         }
     };
-    weights(a.q_weight, e0, wq);
-    weights(a.k_weight, e0, wk);
-    if constexpr (!NEIGHBOURS) {
-        weights(a.q_weight, partner * EPL, wq_other);
-        weights(a.k_weight, partner * EPL, wk_other);
+    fetch(first_token, part);  // on its way while the places are looked up
+
+    // ---- lane i: token i's position, and its row's bytes from the cache's start (-1: no such place; -2: of no sequence) ----
+    int pos = 0;
+    int64_t place = -1;
+    const int64_t mine = first_token + (lane < tokens ? lane : tokens - 1);
+    if constexpr (CACHE) {
+        int b = (int)mine;
+        if (a.q_start) {
+            // the first token's sequence, and how many of the next 64 begin by each of the others
+            const int b0 = sequence_of(a.q_start, a.kv.batch, first_token);
+            b = b0;
+            if constexpr (TOKENS > 1) {
+                // (rows before the first sequence and past the last one are of none: b0 = -1 either way)
+                const bool before = first_token < a.q_start[0];
+                const int from = b0 < 0 ? (before ? 0 : a.kv.batch + 1) : b0 + 1, at = from + lane;
+                const int64_t begins = at <= a.kv.batch ? a.q_start[at] : INT64_MAX;
+#pragma unroll
+                for (int i = 1; i < TOKENS; ++i) {
+                    const int n = __popcll(__ballot(begins <= first_token + i));
+                    if (lane != i || i >= tokens) continue;
+                    // 64 empty sequences in a row: look again from the start
+                    b = n == 64 ? -3 : n == 0 ? b0 : from + n - 1;
+                    if (b == a.kv.batch) b = -1;
+                }
+                uint64_t again = __ballot(b == -3);
+                while (again) {
+                    const int i = __ffsll((unsigned long long)again) - 1;
+                    again &= again - 1;
+                    const int found = sequence_of(a.q_start, a.kv.batch, first_token + i);
+                    if (lane == i) b = found;
+                }
+            }
+        }
+        if (b < 0) {
+            place = -2;
+        } else if (lane < tokens) {
+            const int len = a.kv.length(b);
+            int64_t end = mine + 1;
+            if (a.q_start) end = a.q_start[b + 1] < a.T ? a.q_start[b + 1] : a.T;
+            pos = len - (int)(end - mine);
+            if (pos >= 0 && pos < len) {
+                const int page = a.kv.table[(int64_t)b * a.kv.max_pages + a.kv.page_of(pos)];
+                if ((uint32_t)page < (uint32_t)a.kv.n_pages) place = a.kv.offset(page, pos);
+            }
+        }
     }
+    if (a.position) pos = a.position[mine];
+
+    // weights of this lane's elements and of their partners
+    const int half = a.rot / 2, hl = half / EPL;
+    const bool turned = e0 < a.rot;  // (FAR: all are)
+    const int partner = PAIRS != PART || !turned ? c : c < hl ? c + hl : c - hl;
+    float wq[EPL], wk[EPL], wq_other[EPL], wk_other[EPL];
+    auto weights = [&](const float *src, int first, int second, float (&f)[EPL]) {
+#pragma unroll
+        for (int i = 0; i < EPL; i += EPL / 2)
+#pragma unroll
+            for (int j = 0; j < EPL / 2; j += 2) {
+                const f32x2 v = src ? *reinterpret_cast<const f32x2 *>(src + (i ? second : first) + j) : f32x2{1.0f, 1.0f};
+                f[i + j] = v[0], f[i + j + 1] = v[1];
+            }
+    };
+    weights(a.q_weight, low / SZ, high / SZ, wq);
+    weights(a.k_weight, low / SZ, high / SZ, wk);
+    if constexpr (PAIRS == PART) {
+        weights(a.q_weight, partner * EPL, partner * EPL + EPL / 2, wq_other);
+        weights(a.k_weight, partner * EPL, partner * EPL + EPL / 2, wk_other);
+    }
+    // frequencies of this lane's pairs
+    constexpr int NA = PAIRS == PART ? EPL : EPL / 2;
+    float freq[NA];
+    const int f0 = PAIRS == PART ? (c < hl ? e0 : e0 - half) : c * (EPL / 2);
+#pragma unroll
+    for (int i = 0; i < NA; ++i) freq[i] = turned ? a.inv_freq[f0 + i] : 0.0f;
     auto unpack = [](const u32x4 &v, float (&f)[EPL]) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -136,87 +187,121 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeCall a) {
             }
         }
     };
-    const int groups = (total + HW - 1) / HW;
-    for (int first = part; first < groups; first += BATCH * a.parts) {
-        if (first != part) fetch(first);
+
+    for (int i = 0; i < tokens; ++i) {
+        const int64_t t = first_token + i;
+        const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)place, i), hi = __builtin_amdgcn_readlane((uint32_t)(place >> 32), i);
+        const int64_t cache_off = (int64_t)((uint64_t)hi << 32 | lo);
+        const int p = __builtin_amdgcn_readlane(pos, i);
+        // the angles of this lane's elements at this token
+        float cs[NA], sn[NA];
 #pragma unroll
-        for (int u = 0; u < BATCH; ++u) {
-            const int hg = first + u * a.parts;
-            if (hg >= groups) break;
-            const int h = hg * HW + sub;
-            const bool is_q = h < a.heads, is_v = h >= a.heads + a.kv_heads, mine = h < total;
-            float y[EPL], other[EPL];
-            unpack(x[u], y);
-            if constexpr (!NEIGHBOURS) {
-                u32x4 px;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) px[i] = __shfl(x[u][i], sub * LH + partner);
-                unpack(px, other);
-            }
-            float sq = 0.0f;
-#pragma unroll
-            for (int i = 0; i < EPL; ++i) sq = __builtin_fmaf(y[i], y[i], sq);
-            sq = head_sum<LH>(sq);
-            const bool norm = is_q ? a.q_weight != nullptr : a.k_weight != nullptr;
-            float rs = 1.0f;
+        for (int k = 0; k < NA; ++k) {
+            const double turns = (double)p * ((double)freq[k] * 0.15915494309189533577);
+            const float r = (float)(turns - __builtin_rint(turns));
+            cs[k] = 1.0f, sn[k] = 0.0f;
 #if defined(__HIP_DEVICE_COMPILE__)
-            if (norm) rs = __builtin_amdgcn_rsqf(__builtin_fmaf(sq, 1.0f / D, a.eps));
+            cs[k] = __builtin_amdgcn_cosf(r);
+            sn[k] = __builtin_amdgcn_sinf(r);
+#endif
+            if (PAIRS == PART && c < hl) sn[k] = -sn[k];  // y_i cos - y_j sin; y_j cos + y_i sin
+        }
+        for (int first = part; first < groups; first += BATCH * a.parts) {
+            u32x4 now[BATCH];
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) now[u] = x[u];
+            // the next rows, of this token or the next one
+            if (first + BATCH * a.parts < groups) fetch(t, first + BATCH * a.parts);
+            else if (i + 1 < tokens) fetch(t + 1, part);
+            if (cache_off == -2) continue;  // rows of no sequence
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) {
+                const int hg = first + u * a.parts;
+                if (hg >= groups) break;
+                const int h = hg * HW + sub;
+                const bool is_q = h < a.heads, is_v = h >= a.heads + a.kv_heads, real = h < total;
+                float y[EPL], other[EPL];
+                unpack(now[u], y);
+                if constexpr (PAIRS == PART) {
+                    u32x4 px;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) px[k] = __shfl(now[u][k], sub * LH + partner);
+                    unpack(px, other);
+                }
+                float sq = 0.0f;
+#pragma unroll
+                for (int k = 0; k < EPL; ++k) sq = __builtin_fmaf(y[k], y[k], sq);
+                sq = head_sum<LH>(sq);
+                float rs = 1.0f;
+#if defined(__HIP_DEVICE_COMPILE__)
+                if (is_q ? a.q_weight != nullptr : a.k_weight != nullptr) rs = __builtin_amdgcn_rsqf(__builtin_fmaf(sq, 1.0f / D, a.eps));
 #endif
 #pragma unroll
-            for (int i = 0; i < EPL; ++i) {
-                y[i] = y[i] * rs * (is_q ? wq[i] : wk[i]);
-                if constexpr (!NEIGHBOURS) other[i] = other[i] * rs * (is_q ? wq_other[i] : wk_other[i]);
-            }
-            float out[EPL];
-            if constexpr (NEIGHBOURS) {
-#pragma unroll
-                for (int i = 0; i < EPL / 2; ++i) {
-                    out[2 * i] = y[2 * i] * cs[i] - y[2 * i + 1] * sn[i];
-                    out[2 * i + 1] = y[2 * i + 1] * cs[i] + y[2 * i] * sn[i];
+                for (int k = 0; k < EPL; ++k) {
+                    y[k] = y[k] * rs * (is_q ? wq[k] : wk[k]);
+                    if constexpr (PAIRS == PART) other[k] = other[k] * rs * (is_q ? wq_other[k] : wk_other[k]);
                 }
-            } else {
+                float out[EPL];
+                if constexpr (PAIRS != PART) {
 #pragma unroll
-                for (int i = 0; i < EPL; ++i) out[i] = turned ? y[i] * cs[i] + other[i] * sn[i] : y[i];
-            }
-            u32x4 r;
+                    for (int k = 0; k < EPL / 2; ++k) {
+                        const int i0 = PAIRS == NEAR ? 2 * k : k, i1 = PAIRS == NEAR ? 2 * k + 1 : k + EPL / 2;
+                        out[i0] = y[i0] * cs[k] - y[i1] * sn[k];
+                        out[i1] = y[i1] * cs[k] + y[i0] * sn[k];
+                    }
+                } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) r[i] = BF16 ? pack_bf16x2(out[(2 * i) % EPL], out[(2 * i + 1) % EPL]) : __float_as_uint(out[i]);
-            if (!mine) continue;
-            if (is_q) {
-                *reinterpret_cast<u32x4 *>(a.q_out + t * a.q_out_bytes + (int64_t)h * (D * SZ) + c * 16) = r;
-            } else if constexpr (!CACHE) {
-                *reinterpret_cast<u32x4 *>(a.k_out + t * a.k_out_bytes + (int64_t)(h - a.heads) * (D * SZ) + c * 16) = r;
-            } else if (cache_off >= 0) {
-                const int kh = h - a.heads - (is_v ? a.kv_heads : 0);
-                unsigned char *base = const_cast<unsigned char *>(is_v ? a.kv.v : a.kv.k);
-                *reinterpret_cast<u32x4 *>(base + cache_off + kh * a.kv.head_bytes + c * 16) = is_v ? x[u] : r;
+                    for (int k = 0; k < EPL; ++k) out[k] = turned ? y[k] * cs[k] + other[k] * sn[k] : y[k];
+                }
+                u32x4 r;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) r[k] = BF16 ? pack_bf16x2(out[(2 * k) % EPL], out[(2 * k + 1) % EPL]) : __float_as_uint(out[k]);
+                if (!real) continue;
+                if (is_q) {
+                    store(a.q_out + t * a.q_out_bytes + (int64_t)h * (D * SZ), r);
+                } else if constexpr (!CACHE) {
+                    store(a.k_out + t * a.k_out_bytes + (int64_t)(h - a.heads) * (D * SZ), r);
+                } else if (cache_off >= 0) {
+                    const int kh = h - a.heads - (is_v ? a.kv_heads : 0);
+                    unsigned char *base = const_cast<unsigned char *>(is_v ? a.kv.v : a.kv.k);
+                    store(base + cache_off + kh * a.kv.head_bytes, is_v ? now[u] : r);
+                }
             }
         }
     }
 }
 
+template <bool BF16, int D, bool CACHE, Pairs PAIRS>
+static void start(const RopeCall &a, int tokens, unsigned blocks, hipStream_t st) {
+    if (tokens == 1) qk_norm_rope_kernel<BF16, D, CACHE, PAIRS, 1><<<dim3(blocks), dim3(256), 0, st>>>(a);
+    else qk_norm_rope_kernel<BF16, D, CACHE, PAIRS, ROPE_TOKENS><<<dim3(blocks), dim3(256), 0, st>>>(a);
+}
+
 template <bool BF16, int D, bool CACHE>
-static void start(const RopeCall &a, bool neighbours, unsigned blocks, hipStream_t st) {
-    if (neighbours) qk_norm_rope_kernel<BF16, D, CACHE, true><<<dim3(blocks), dim3(256), 0, st>>>(a);
-    else qk_norm_rope_kernel<BF16, D, CACHE, false><<<dim3(blocks), dim3(256), 0, st>>>(a);
+static void start(const RopeCall &a, bool neighbours, int tokens, unsigned blocks, hipStream_t st) {
+    if (neighbours) start<BF16, D, CACHE, NEAR>(a, tokens, blocks, st);
+    else if (a.rot == D) start<BF16, D, CACHE, FAR>(a, tokens, blocks, st);
+    else start<BF16, D, CACHE, PART>(a, tokens, blocks, st);
 }
 
 int launch_qk_norm_rope(RopeCall a, bool bf16, int D, bool neighbours, hipStream_t st) {
     const bool cache = a.k_out == nullptr;
     const int lanes = D * (bf16 ? 2 : 4) / 16, groups = (int)ceil_div(a.heads + (cache ? 2 : 1) * a.kv_heads, 64 / lanes);
-    // Waves per token: one per head group while they all fit the chip at once, then four groups a wave.
-    int64_t parts = ceil_div(8192, a.T);
-    if (parts < ceil_div(groups, 4)) parts = ceil_div(groups, 4);
+    // Few tokens: waves for every four head groups, down to one, while the chip has room.  Many: a wave takes all head groups of
+    // ROPE_TOKENS tokens.
+    const int tokens = a.T * ceil_div(groups, 4) >= ROPE_MANY ? ROPE_TOKENS : 1;
+    int64_t parts = tokens > 1 ? 1 : ceil_div(8192, a.T);
+    if (tokens == 1 && parts < ceil_div(groups, 4)) parts = ceil_div(groups, 4);
     a.parts = (int)(parts < groups ? parts : groups);
-    const int64_t blocks = ceil_div(a.T * a.parts, 4);
+    const int64_t blocks = ceil_div(ceil_div(a.T, tokens) * a.parts, 4);
     if (blocks >= ATTN_MOST_BLOCKS) return C2R_ERR_UNSUPPORTED;
     const unsigned n = (unsigned)blocks;
     if (bf16) {
-        if (D == 128) cache ? start<true, 128, true>(a, neighbours, n, st) : start<true, 128, false>(a, neighbours, n, st);
-        else cache ? start<true, 64, true>(a, neighbours, n, st) : start<true, 64, false>(a, neighbours, n, st);
+        if (D == 128) cache ? start<true, 128, true>(a, neighbours, tokens, n, st) : start<true, 128, false>(a, neighbours, tokens, n, st);
+        else cache ? start<true, 64, true>(a, neighbours, tokens, n, st) : start<true, 64, false>(a, neighbours, tokens, n, st);
     } else {
-        if (D == 128) cache ? start<false, 128, true>(a, neighbours, n, st) : start<false, 128, false>(a, neighbours, n, st);
-        else cache ? start<false, 64, true>(a, neighbours, n, st) : start<false, 64, false>(a, neighbours, n, st);
+        if (D == 128) cache ? start<false, 128, true>(a, neighbours, tokens, n, st) : start<false, 128, false>(a, neighbours, tokens, n, st);
+        else cache ? start<false, 64, true>(a, neighbours, tokens, n, st) : start<false, 64, false>(a, neighbours, tokens, n, st);
     }
     return launch_status();
 }
