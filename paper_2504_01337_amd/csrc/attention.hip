@@ -78,7 +78,7 @@ size_t attention_workspace_bytes(int64_t T, int D, int heads, int kv_heads, int 
     // the most rows x parts that attn_parts() gives where it gives more than one part: `blocks` blocks become at most
     // target + blocks, and each has at most per_block rows
     const int64_t rows = T * heads;
-    auto bound = [rows](int64_t target, int64_t per_block) { return rows < target * per_block ? target * per_block + rows : 0; };
+    auto bound = [rows](int64_t target, int64_t per_block) { return rows <= target * per_block ? target * per_block + rows : 0; };
     if (max_q_len <= 0)
         return round_up((size_t)bound(ATTN_DECODE_EVEN_BLOCKS, heads / kv_heads < 16 ? heads / kv_heads : 16) * (size_t)(D + 2) * 4, 256);
     const int64_t tile = bound(ATTN_TILE_BLOCKS, ATTN_TILE_ROWS), full = bound(ATTN_ROWS_BLOCKS, ATTN_ROWS_ROWS);
@@ -240,7 +240,11 @@ extern "C" int c2r_attention_prefill(const void *q, int64_t q_stride, int64_t T,
     const int64_t blocks = cache->batch * cache->kv_heads * ceil_div((int64_t)a.max_q * a.group, per_block);
     if ((int64_t)a.max_q * a.group >= (1ll << 31)) return C2R_ERR_UNSUPPORTED;
     const int64_t tiles = attn_max_tiles(a, bf16 ? 64 : 16, ceil_div(per_block, a.group) + 1, longest(cache, max_kv_len));
-    attn_split(a, tiles, bf16 ? prompt_parts(blocks, tiles, T * heads, (int)cache->head_dim) : attn_parts(blocks, tiles, ATTN_ROWS_BLOCKS, ATTN_ROWS_TILES));
+    int64_t parts = bf16 ? prompt_parts(blocks, tiles, T * heads, (int)cache->head_dim) : attn_parts(blocks, tiles, ATTN_ROWS_BLOCKS, ATTN_ROWS_TILES);
+    // (partial results are laid out by rows of q: rows that no sequence has, or past its max_q_len, take their room, too, and
+    // more parts than the workspace query foresees are not made)
+    const int64_t room = (bf16 ? ATTN_TILE_BLOCKS : ATTN_ROWS_BLOCKS) * per_block / (T * heads) + 1;
+    attn_split(a, tiles, parts < room ? parts : room);
     if (blocks * a.splits >= ATTN_MOST_BLOCKS) return C2R_ERR_UNSUPPORTED;
     rc = place_parts(a, (int)cache->head_dim, ws, ws_bytes);
     if (rc != C2R_OK) return rc;

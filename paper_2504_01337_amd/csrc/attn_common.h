@@ -87,14 +87,10 @@ struct KeyTiles {
     }
 };
 
-// A tile [base, base + KT) that every query of p_min .. p_max sees whole, and one that some of them see some of.
+// A tile [base, base + KT) that every query of p_min .. p_max sees whole.
 template <int KT>
 __device__ __forceinline__ bool tile_whole(const AttnCall &a, int base, int p_min, int p_max) {
     return base + KT - 1 <= p_min && (!a.window || base > p_max - a.window || base + KT <= a.sinks);
-}
-template <int KT>
-__device__ __forceinline__ bool tile_seen(const AttnCall &a, int base, int p_min, int p_max) {
-    return base <= p_max && (!a.window || base + KT - 1 > p_min - a.window || base < a.sinks);
 }
 
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }

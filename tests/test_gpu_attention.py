@@ -372,6 +372,19 @@ def test_prefill_rows_past_the_stated_most_are_untouched(c2r, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [8, 9000, 40000, 70000])
+def test_prefill_with_many_rows_of_no_sequence(c2r, dtype, T):
+    """Rows that are there for a larger batch: the workspace that is asked for holds the keys' parts, however many rows there are."""
+    rng = np.random.default_rng(12)
+    bt = Batch(c2r, rng, dtype, 64, 1, 16, [3000], [8])
+    q = _randn(rng, T, 1, 64, dtype=dtype)
+    out = torch.full_like(q, 7.0)
+    c2r.attention_prefill(q, bt.cache, bt.q_start, 8, out=out)
+    _check_attention(out[:8], q[:8], bt, dtype, 64 ** -0.5, 0, 0)
+    assert (out[8:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("junk", [float("nan"), float("inf"), -float("inf"), -3.3895e38])
 @pytest.mark.parametrize("context", [0, 1500])                       # one part, and keys that are split
 def test_prefill_hidden_junk(c2r, dtype, junk, context):
