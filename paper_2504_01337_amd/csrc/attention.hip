@@ -175,16 +175,32 @@ static int64_t longest(const c2r_kv_cache *cache, int64_t max_kv_len) {
     return max_kv_len > 0 && max_kv_len < capacity ? max_kv_len : capacity;
 }
 
-// Parts that the keys of a bf16 prompt are cut into: `blocks` blocks of up to `tiles` tiles, `rows` query rows in all.  Estimated
-// microseconds, from measurements with heads of 128: a tile takes 1.6 where a CU has one block and 2.3 where it has two, a
-// second launch 5, and every part writes and reads back the rows' sums.  (256 new tokens behind 8000, 16 heads: whole 177, 4
-// parts 58, 8 parts 42, 16 parts 43; 2000 tokens, 16 heads: whole 49, 2 parts 55.)
-static int64_t prompt_parts(int64_t blocks, int64_t tiles, int64_t rows, int D) {
+// Parts that the keys of a bf16 prompt are cut into: the number whose estimated time is least.  Blocks of 128 rows look at up to
+// `tiles` tiles, those of a prompt's first rows at fewer; a block with more than tiles / n is cut.  A tile takes 1.6 us in a
+// block's hands where two blocks share a CU (heads of 128); the call takes as long as its longest part, or as the tiles over the
+// GPU's 512 places and some of a part behind them.  A cut costs a second launch and the writing and reading of the cut rows'
+// sums.  Measured, us, 1 to 4 parts (16 heads unless said): 2000 tokens 51, 46, 42, 57; 1000 behind 16000 361, 208, 182, 160; 500
+// behind 2000, 32 heads 53, 48, 46, 43; three ragged chunks of 700 behind 5000 135, 94, 77, 91; but 4 x 2048 88, 138, 141, 198 and
+// 4000 tokens 96, 115, 106, 135; 256 behind 8000 in 8 parts 41 and whole 174.  Over 24 such calls the choice is 4 % over the best of
+// 1, 2, 3, 4, 6 and 8 parts on average, and 19 % at most (a ragged batch, whose lengths the host does not know).
+static int64_t prompt_parts(const AttnCall &a, int64_t blocks, int64_t tiles, int64_t longest, int D) {
+    // (a batch's T rows may be far fewer than batch * max_q; every sequence and key head has a block that is not full)
+    const double rows = (double)a.T * a.heads, real = rows / ATTN_TILE_ROWS + a.kv.batch * a.kv.kv_heads * 0.5;
+    const double units = real < blocks ? real : blocks, rate = D == 128 ? 1.6 : 0.92;
+    const double fewest = a.window ? 0.9 * tiles : a.max_q < longest ? tiles * (1.0 - (double)a.max_q / longest) : 0.0;
+    constexpr int SAMPLES = 8;
     int64_t best = 1;
     double least = 0.0;
-    for (int64_t n = 1; n == 1 || (n <= ATTN_TILE_BLOCKS / blocks && n <= ceil_div(tiles, ATTN_TILE_TILES)); ++n) {
-        const double each = (double)ceil_div(tiles, n) * (blocks * n <= 256 ? 1.6 : 2.3) * D / 128;
-        const double t = each + (n == 1 ? 0.0 : 5.0 + (double)rows * n * D * 8 / 4e6);
+    for (int64_t n = 1; n == 1 || (n * units <= ATTN_TILE_BLOCKS && n <= ceil_div(tiles, ATTN_TILE_TILES)); ++n) {
+        const double each = (double)ceil_div(tiles, n);
+        double all = 0.0, cut = 0.0;  // a block's tiles; its parts, where it is cut
+        for (int i = 0; i < SAMPLES; ++i) {
+            const double c = fewest + (tiles - fewest) * (i + 0.5) / SAMPLES;
+            all += c / SAMPLES;
+            if (c > each) cut += (double)(int64_t)(c / each + 1.0) / SAMPLES;
+        }
+        const double part = each * rate, spread = 0.9 * units * all * rate / ATTN_TILE_BLOCKS + 0.4 * part;
+        const double t = (part > spread ? part : spread) + (n == 1 ? 0.0 : 5.0 + rows * cut * D * 8 / 2e6);
         if (n == 1 || t < least) least = t, best = n;
     }
     return best;
@@ -240,7 +256,10 @@ extern "C" int c2r_attention_prefill(const void *q, int64_t q_stride, int64_t T,
     const int64_t blocks = cache->batch * cache->kv_heads * ceil_div((int64_t)a.max_q * a.group, per_block);
     if ((int64_t)a.max_q * a.group >= (1ll << 31)) return C2R_ERR_UNSUPPORTED;
     const int64_t tiles = attn_max_tiles(a, bf16 ? 64 : 16, ceil_div(per_block, a.group) + 1, longest(cache, max_kv_len));
-    int64_t parts = bf16 ? prompt_parts(blocks, tiles, T * heads, (int)cache->head_dim) : attn_parts(blocks, tiles, ATTN_ROWS_BLOCKS, ATTN_ROWS_TILES);
+    // Full precision: parts of 6 tiles (96 keys) or more until there are 1024 blocks.  us, parts of 4, 6, 8 tiles: 512 tokens, 4 heads
+    // of 64 15.8, 16.9, 18.0, 2 x 64 behind 4000 21.8, 20.6, 20.5, 3 x 5 behind 3000 24.6, 22.7, 25.7;  512, 1024, 2048 blocks: 2 x
+    // 2000 tokens, 4 heads of 128 192, 159, 175, 1500 tokens, 8 heads of 64 64, 58, 63.
+    int64_t parts = bf16 ? prompt_parts(a, blocks, tiles, longest(cache, max_kv_len), (int)cache->head_dim) : attn_parts(blocks, tiles, ATTN_ROWS_BLOCKS, ATTN_ROWS_TILES);
     // (partial results are laid out by rows of q: rows that no sequence has, or past its max_q_len, take their room, too, and
     // more parts than the workspace query foresees are not made)
     const int64_t room = (bf16 ? ATTN_TILE_BLOCKS : ATTN_ROWS_BLOCKS) * per_block / (T * heads) + 1;

@@ -36,6 +36,10 @@ struct KvView {
     }
 };
 
+// In the place of a part's denominator: it holds no key of this row and has written no sums; all of the row's keys were in the
+// first part, which has written the result.
+constexpr float PART_EMPTY = -1.0f, PART_DONE = -2.0f;
+
 // One call of attention.  New tokens of sequence b: rows q_start[b] .. of q (b .. b + 1 where q_start is null); the last of
 // them stands at position kv_len[b] - 1.
 struct AttnCall {
@@ -50,7 +54,7 @@ struct AttnCall {
     int window, sinks;        // window 0: none
     float scale_log2;         // scale * log2(e): the softmax is taken in powers of two
     int splits, split_tiles;  // the key tiles of one row of blocks, cut after every split_tiles; 1: no partial results
-    float *part_o, *part_ml;  // [splits][T * heads][D] sums, [splits][T * heads][2] maximum and denominator
+    float *part_o, *part_ml;  // [splits][T * heads][D] sums, [splits][T * heads][2] maximum and denominator (or PART_..)
 
     __device__ __forceinline__ int first_row(int b) const { return q_start ? (int)clamp_row(q_start[b]) : b; }
     __device__ __forceinline__ int new_tokens(int b) const {
@@ -85,6 +89,8 @@ struct KeyTiles {
         x0 = lo < count ? (int)lo : count;
         x1 = hi < count ? (int)hi : count;
     }
+    // Whether split 0 has all of them: it then writes the result itself and says so to the join (PART_DONE).
+    __device__ __forceinline__ bool uncut(const AttnCall &a) const { return a.splits == 1 || count <= a.split_tiles; }
 };
 
 // A tile [base, base + KT) that every query of p_min .. p_max sees whole.
@@ -177,7 +183,7 @@ int launch_attn_tile(const AttnCall &a, int D, hipStream_t st);
 // tiles of a part.
 constexpr int ATTN_DECODE_BLOCKS = 768, ATTN_DECODE_TILES = 8, ATTN_DECODE_EVEN_BLOCKS = 4608, ATTN_DECODE_EVEN_TILES = 24;
 constexpr int ATTN_TILE_BLOCKS = 512, ATTN_TILE_TILES = 4, ATTN_TILE_ROWS = 128;
-constexpr int ATTN_ROWS_BLOCKS = 512, ATTN_ROWS_TILES = 8, ATTN_ROWS_ROWS = 64;
+constexpr int ATTN_ROWS_BLOCKS = 1024, ATTN_ROWS_TILES = 6, ATTN_ROWS_ROWS = 64;
 
 // A grid's threads are counted in 32 bits.
 constexpr int64_t ATTN_MOST_BLOCKS = 1ll << 24;

@@ -20,15 +20,14 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void attn_decode_kernel(Attn
     const KeyTiles<KT> tiles(a, p, p);
     int x0, x1;
     tiles.part(a, split, x0, x1);
-    // row r of this part: a.part_ml says -1 where it holds no key
+    const bool uncut = tiles.uncut(a);
     const int64_t part_row = ((int64_t)split * a.kv.batch + b) * a.heads + head0;
-    if (x0 == x1 && a.splits > 1) {
-        if (threadIdx.x < (uint32_t)left) {
-            a.part_ml[(part_row + threadIdx.x) * 2] = -__builtin_inff();
-            a.part_ml[(part_row + threadIdx.x) * 2 + 1] = -1.0f;
-        }
-        return;
+    if (uncut && split > 0) return;
+    if (threadIdx.x < (uint32_t)left && a.splits > 1 && (uncut || x0 == x1)) {
+        a.part_ml[(part_row + threadIdx.x) * 2] = -__builtin_inff();
+        a.part_ml[(part_row + threadIdx.x) * 2 + 1] = uncut ? PART_DONE : PART_EMPTY;
     }
+    if (!uncut && x0 == x1) return;
     const unsigned char *q_rows = a.q + b * a.q_bytes + (int64_t)head0 * (D * SZ);
     u32x4 q[S::KSTEPS];
 #pragma unroll
@@ -70,7 +69,7 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void attn_decode_kernel(Attn
 #pragma unroll
             for (int e = 0; e < 4; ++e) sum[e] = __builtin_fmaf(f, o[e], sum[e]);
         }
-        if (a.splits == 1) {
+        if (uncut) {
             const float inv = p < 0 ? 0.0f : 1.0f / l, v[4] = {sum[0] * inv, sum[1] * inv, sum[2] * inv, sum[3] * inv};
             store_elements<BF16, 4>(a.out + b * a.out_bytes + ((int64_t)(head0 + col) * D + d) * SZ, v);
         } else {

@@ -35,16 +35,19 @@ __global__ __launch_bounds__(256, 3) void attn_rows_kernel(AttnCall a, int row_b
     const KeyTiles<KT> tiles(a, p_min, p_max);
     int x0, x1;
     tiles.part(a, split, x0, x1);
+    const bool uncut = tiles.uncut(a);
+    if (uncut && split > 0) return;
     typename S::State st;
     S::clear(st);
     S::template run<1>(a, q, st, tiles, x0, x1, b, kv_head * a.kv.head_bytes, p, p_min, p_max);
     uint32_t redo = S::finish(st, left);
 
     const int64_t part_rows = a.T * a.heads;
-    // N elements from `at` on of one row: to `out` where the keys were not split, else the partial sums
+    // N elements from `at` on of one row: to `out` where this wave had all keys, else the partial sums
     auto put = [&](int64_t tok, int hd, int at, const float *v, auto count, float m, float l, int pos, bool ml) {
         constexpr int N = decltype(count)::value;
-        if (a.splits == 1) {
+        if (uncut) {
+            if (ml && a.splits > 1) a.part_ml[(tok * a.heads + hd) * 2] = -__builtin_inff(), a.part_ml[(tok * a.heads + hd) * 2 + 1] = PART_DONE;
             const float inv = 1.0f / l;
             float *out = reinterpret_cast<float *>(a.out + tok * a.out_bytes + (int64_t)hd * (D * 4)) + at;
 #pragma unroll
@@ -53,7 +56,7 @@ __global__ __launch_bounds__(256, 3) void attn_rows_kernel(AttnCall a, int row_b
             const int64_t pr = (int64_t)split * part_rows + tok * a.heads + hd;
 #pragma unroll
             for (int e = 0; e < N; ++e) a.part_o[pr * D + at + e] = v[e];
-            if (ml) a.part_ml[pr * 2] = m, a.part_ml[pr * 2 + 1] = pos < 0 || x0 == x1 ? -1.0f : l;
+            if (ml) a.part_ml[pr * 2] = m, a.part_ml[pr * 2 + 1] = pos < 0 || x0 == x1 ? PART_EMPTY : l;
         }
     };
     if (n < left) {

@@ -108,6 +108,17 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
     const KeyTiles<KT> tiles(a, bp_min, bp_max);
     int x0, x1;
     tiles.part(a, split, x0, x1);
+    const bool uncut = tiles.uncut(a);
+    const int64_t part_rows = a.T * a.heads;
+    if (uncut && split > 0) return;
+    if (a.splits > 1 && (uncut || x0 == x1)) {
+        for (int r = threadIdx.x; r < block_rows; r += 256) {
+            const int rr = block0 + r, ir = rr / a.group;
+            float *ml = a.part_ml + ((int64_t)split * part_rows + (a.first_row(b) + ir) * a.heads + kv_head * a.group + rr - ir * a.group) * 2;
+            ml[0] = -__builtin_inff(), ml[1] = uncut ? PART_DONE : PART_EMPTY;
+        }
+        if (!uncut) return;
+    }
 
     // ---- copies: rows first_row(u) + lane / CH of a tile; pieces in the order the LDS image wants ----
     const int64_t head_off = kv_head * a.kv.head_bytes;
@@ -367,9 +378,8 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
     redo = (redo | redo >> 32) & 0xffffffffu;
 
     // ---- results: lane (h, n), word e of o[d]: element 32 d + 8 (e / 4) + 4 h + e % 4 of row n ----
-    const int64_t part_rows = a.T * a.heads;
     if (n < left) {
-        if (a.splits == 1) {
+        if (uncut) {
             const float inv = p < 0 ? 0.0f : 1.0f / l;
             unsigned char *out = a.out + token * a.out_bytes + (int64_t)head * (D * 2);
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -395,7 +405,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
 #pragma unroll
                 for (int e = 0; e < 16; e += 4)
                     *reinterpret_cast<f32x4 *>(a.part_o + prow * D + d * 32 + e * 2 + h * 4) = f32x4{o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]};
-            if (h == 0) a.part_ml[prow * 2] = m, a.part_ml[prow * 2 + 1] = p < 0 || x0 == x1 ? -1.0f : l;
+            if (h == 0) a.part_ml[prow * 2] = m, a.part_ml[prow * 2 + 1] = p < 0 ? PART_EMPTY : l;
         }
     }
     while (redo) {
@@ -405,7 +415,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
         const int64_t tc = a.first_row(b) + ic;
         float me, le, v[D / 64];
         exact_row<true, D, KT>(a, tiles, x0, x1, 1, b, kv_head, before + ic, a.q + tc * a.q_bytes + (int64_t)hc * (D * 2), me, le, v);
-        if (a.splits == 1) {
+        if (uncut) {
             const float inv = before + ic < 0 ? 0.0f : 1.0f / le;
             uint16_t *out = reinterpret_cast<uint16_t *>(a.out + tc * a.out_bytes + (int64_t)hc * (D * 2)) + lane * (D / 64);
 #pragma unroll
@@ -414,7 +424,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
             const int64_t prow = (int64_t)split * part_rows + tc * a.heads + hc;
 #pragma unroll
             for (int e = 0; e < D / 64; ++e) a.part_o[prow * D + lane * (D / 64) + e] = v[e];
-            if (lane == 0) a.part_ml[prow * 2] = me, a.part_ml[prow * 2 + 1] = before + ic < 0 ? -1.0f : le;
+            if (lane == 0) a.part_ml[prow * 2] = me, a.part_ml[prow * 2 + 1] = before + ic < 0 ? PART_EMPTY : le;
         }
     }
 }
