@@ -7,7 +7,13 @@
 // within 16 keys, lane half h holds keys 4h..4h+3 and 8+4h..8+4h+3, and V's rows are counted in that order by reading them
 // from LDS transposed (ds_read_b64_tr_b16: 4 keys of one element per lane).  Scores and weights never pass through LDS.
 // K and V tiles are copied straight into LDS, the next pair in flight while one is worked on, one barrier per tile; a row's
-// 16-byte pieces are stored at piece ^ row so that neither read meets on a bank.
+// 16-byte pieces are stored at piece ^ key(row) so that neither read meets on a bank.
+//
+// Bound by issue: a tile of 128 rows is 32 products a wave and some 220 vector instructions, and the chip is power limited under
+// both (1.9 GHz).  Heads of 128: one prompt of 8192 tokens, 16 heads 290 us (950 TFLOP/s of visible pairs; the library's product
+// of 8192^3 reaches 1143); 4 prompts of 2048 88 us (780); 16000 tokens through a window of 2048 with 16 sinks 295 to 320 (790 to 860);
+// heads of 64, 4 x 2048 51 us (670).  128 rows to a block: K and V are read from LDS by four waves, and 64 rows to a wave, with half
+// those reads, need more registers than stay out of the accumulation half (slower).
 #include "attn_common.h"
 
 namespace c2r {
@@ -275,8 +281,8 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
         if (READS) __builtin_amdgcn_sched_group_barrier(DS_READ, READS, 0); \
         if (OTHERS) __builtin_amdgcn_sched_group_barrier(VALU, OTHERS, 0);  \
     }
-        // (Copies of the next tile go out in halves after the first two stretches: all at once, right behind the barrier, they
-        // wait for each other: 761 cycles of a tile's 3300.)
+        // (Copies of the next tile go out in halves after the first two stretches: all at once, right behind the barrier, the
+        // waves wait for each other's.  With the maximum moved behind the products, 4 x 2048 tokens 101 -> 94 us.)
         // Scores are taken against m, a whole number near the largest score of a row's first tile that has any, and moved on
         // where a later score is over 2^30 above it: bf16 has the exponents of fp32, so weights of 2^30 are as good as weights
         // of 1, and nothing waits for a maximum.  (A score 2^127 above the ones before it overflows, which the check of the
