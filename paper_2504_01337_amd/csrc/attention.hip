@@ -253,8 +253,12 @@ extern "C" int c2r_attention_prefill(const void *q, int64_t q_stride, int64_t T,
     a.max_q = (int)(max_q_len < T ? max_q_len : T);
     const bool bf16 = cache->dtype == C2R_BF16;
     const int64_t per_block = bf16 ? ATTN_TILE_ROWS : ATTN_ROWS_ROWS;
-    const int64_t blocks = cache->batch * cache->kv_heads * ceil_div((int64_t)a.max_q * a.group, per_block);
-    if ((int64_t)a.max_q * a.group >= (1ll << 31)) return C2R_ERR_UNSUPPORTED;
+    if (T * a.group >= (1ll << 31)) return C2R_ERR_UNSUPPORTED;
+    const int64_t each = ceil_div((int64_t)a.max_q * a.group, per_block), by_rows = T * a.group / per_block + cache->batch;
+    a.by_rows = each * cache->batch > ATTN_BY_ROWS * by_rows;
+    const int64_t blocks = cache->kv_heads * (a.by_rows ? by_rows : each * cache->batch);
+    if (blocks >= ATTN_MOST_BLOCKS) return C2R_ERR_UNSUPPORTED;
+    a.row_blocks = (int)(a.by_rows ? by_rows : each);
     const int64_t tiles = attn_max_tiles(a, bf16 ? 64 : 16, ceil_div(per_block, a.group) + 1, longest(cache, max_kv_len));
     // Full precision: parts of 6 tiles (96 keys) or more until there are 1024 blocks.  us, parts of 4, 6, 8 tiles: 512 tokens, 4 heads
     // of 64 15.8, 16.9, 18.0, 2 x 64 behind 4000 21.8, 20.6, 20.5, 3 x 5 behind 3000 24.6, 22.7, 25.7;  512, 1024, 2048 blocks: 2 x
@@ -263,6 +267,8 @@ extern "C" int c2r_attention_prefill(const void *q, int64_t q_stride, int64_t T,
     // (partial results are laid out by rows of q: rows that no sequence has, or past its max_q_len, take their room, too, and
     // more parts than the workspace query foresees are not made)
     const int64_t room = (bf16 ? ATTN_TILE_BLOCKS : ATTN_ROWS_BLOCKS) * per_block / (T * heads) + 1;
+    // (the join has blocks for max_q rows of every sequence)
+    if (ceil_div((int64_t)a.max_q * heads, 4) * cache->batch > ATTN_JOIN_BLOCKS) parts = 1;
     attn_split(a, tiles, parts < room ? parts : room);
     if (blocks * a.splits >= ATTN_MOST_BLOCKS) return C2R_ERR_UNSUPPORTED;
     rc = place_parts(a, (int)cache->head_dim, ws, ws_bytes);

@@ -36,6 +36,23 @@ struct KvView {
     }
 };
 
+// How many i of 0 .. n - 1 are `below`, which are the first ones: the wave looks at 64 evenly spread ones, then at the 64 steps
+// between two of them, ...
+template <class F>
+__device__ __forceinline__ int count_first(int n, const F &below) {
+    int lo = 0;  // the count lies in lo .. lo + n
+    const int lane = lane_id();
+    while (n > 0) {
+        const int step = (n + 63) / 64, at = lo + (lane + 1) * step - 1;  // last one of each of 64 runs
+        const int runs = __popcll(__ballot(at < lo + n && below(at)));
+        lo += runs * step;
+        const int rest = n - runs * step;
+        n = rest < step - 1 ? rest : step - 1;
+        if (step == 1) break;
+    }
+    return lo;
+}
+
 // In the place of a part's denominator: it holds no key of this row and has written no sums; all of the row's keys were in the
 // first part, which has written the result.
 constexpr float PART_EMPTY = -1.0f, PART_DONE = -2.0f;
@@ -54,6 +71,10 @@ struct AttnCall {
     int window, sinks;        // window 0: none
     float scale_log2;         // scale * log2(e): the softmax is taken in powers of two
     int splits, split_tiles;  // the key tiles of one row of blocks, cut after every split_tiles; 1: no partial results
+    // Prompts: blocks of rows for every key head and part.  by_rows: counted through all sequences, T * group / BM + batch of them;
+    // else as many for each sequence as max_q needs.
+    int row_blocks;
+    bool by_rows;
     float *part_o, *part_ml;  // [splits][T * heads][D] sums, [splits][T * heads][2] maximum and denominator (or PART_..)
 
     __device__ __forceinline__ int first_row(int b) const { return q_start ? (int)clamp_row(q_start[b]) : b; }
@@ -63,6 +84,23 @@ struct AttnCall {
         return n > 0 ? (int)n : 0;
     }
     __device__ __forceinline__ int64_t clamp_row(int32_t r) const { return r < 0 ? 0 : (int64_t)r > T ? T : r; }
+    // Block x of a key head's and part's: sequence b, block rb of its rows, a sequence's last (longest) ones first.  False: there
+    // is none.
+    // by_rows: sequence b has the numbers from q_start[b] * group / BM + b on, which are enough: floor(x + y) + 1 >= floor(x) +
+    // ceil(y).
+    template <int BM>
+    __device__ __forceinline__ bool block_of(int x, int &b, int &rb) const {
+        if (!by_rows) {
+            b = x % kv.batch, rb = row_blocks - 1 - x / kv.batch;
+            return true;
+        }
+        auto begin = [&](int i) { return (int)(clamp_row(q_start[i]) * group / BM) + i; };
+        b = count_first(kv.batch, [&](int i) { return begin(i) <= x; }) - 1;
+        if (b < 0) return false;
+        const int64_t rows = (int64_t)min(new_tokens(b), max_q) * group;
+        rb = (int)((rows + BM - 1) / BM) - 1 - (x - begin(b));
+        return rb >= 0;
+    }
     // Whether the query at position p sees key j.
     __device__ __forceinline__ bool sees(int p, int j) const { return j <= p && (!window || j > p - window || j < sinks); }
 };
@@ -184,6 +222,15 @@ int launch_attn_tile(const AttnCall &a, int D, hipStream_t st);
 constexpr int ATTN_DECODE_BLOCKS = 768, ATTN_DECODE_TILES = 8, ATTN_DECODE_EVEN_BLOCKS = 4608, ATTN_DECODE_EVEN_TILES = 24;
 constexpr int ATTN_TILE_BLOCKS = 512, ATTN_TILE_TILES = 4, ATTN_TILE_ROWS = 128;
 constexpr int ATTN_ROWS_BLOCKS = 1024, ATTN_ROWS_TILES = 6, ATTN_ROWS_ROWS = 64;
+
+// Rows are counted through all sequences where that makes less than half of the blocks: a batch of a few chunks among single
+// tokens, whose other blocks would find no row.  us by rows and with as many blocks for each sequence: 32 / 8 heads, one chunk of
+// 1500 and 255 single tokens behind 1000 208 and 351, the chunk last 220 and 358; 500 behind 8000 and 15 singles 101 and 135; 2 of
+// 1000 and 30 of 20, 16 heads 27 and 27, but with the long ones last, whose blocks then start last, 39 and 29; not so many idle ones:
+// 4 x 2048 93 and 85, five ragged chunks 83.4 and 81.3.
+constexpr int ATTN_BY_ROWS = 2;
+// Blocks of a join from which on keys are not cut: nearly all of them would find nothing to do.
+constexpr int64_t ATTN_JOIN_BLOCKS = 1 << 17;
 
 // A grid's threads are counted in 32 bits.
 constexpr int64_t ATTN_MOST_BLOCKS = 1ll << 24;

@@ -9,17 +9,18 @@
 namespace c2r {
 
 template <int D>
-__global__ __launch_bounds__(256, 3) void attn_rows_kernel(AttnCall a, int row_blocks) {
+__global__ __launch_bounds__(256, 3) void attn_rows_kernel(AttnCall a) {
     using S = Stream<false, D>;
     constexpr int KT = S::KT;
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, n = lane & 15;
-    // blocks: split fastest, then key heads, row blocks, sequences
+    // blocks: split fastest, then key heads, rows
     int64_t id = blockIdx.x;
     const int split = (int)(id % a.splits);
     id /= a.splits;
     const int kv_head = (int)(id % a.kv.kv_heads);
     id /= a.kv.kv_heads;
-    const int rb = (int)(id % row_blocks), b = (int)(id / row_blocks);
+    int b, rb;
+    if (!a.block_of<ATTN_ROWS_ROWS>((int)id, b, rb)) return;
     const int fresh = a.new_tokens(b), before = a.kv.length(b) - fresh, rows = min(fresh, a.max_q) * a.group;
     const int row0 = (rb * 4 + wave) * 16, left = min(rows - row0, 16);
     if (left <= 0) return;
@@ -81,10 +82,9 @@ __global__ __launch_bounds__(256, 3) void attn_rows_kernel(AttnCall a, int row_b
 }
 
 int launch_attn_rows_f32(const AttnCall &a, int D, hipStream_t st) {
-    const int row_blocks = (int)ceil_div((int64_t)a.max_q * a.group, ATTN_ROWS_ROWS);
-    const dim3 grid((unsigned)((int64_t)a.splits * a.kv.kv_heads * row_blocks * a.kv.batch)), block(256);
-    if (D == 128) attn_rows_kernel<128><<<grid, block, 0, st>>>(a, row_blocks);
-    else attn_rows_kernel<64><<<grid, block, 0, st>>>(a, row_blocks);
+    const dim3 grid((unsigned)((int64_t)a.splits * a.kv.kv_heads * a.row_blocks * (a.by_rows ? 1 : a.kv.batch))), block(256);
+    if (D == 128) attn_rows_kernel<128><<<grid, block, 0, st>>>(a);
+    else attn_rows_kernel<64><<<grid, block, 0, st>>>(a);
     const int rc = launch_status();
     return rc == C2R_OK && a.splits > 1 ? launch_attn_join(a, false, D, st) : rc;
 }

@@ -82,7 +82,7 @@ __device__ __forceinline__ float add_halves(float v) {
 // one page: one look-up and one scalar address.  Working out every lane's page takes as many vector instructions per tile as
 // the softmax.
 template <int D, bool ALIGNED>
-__global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_blocks) {
+__global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a) {
     using T = TileShape<D>;
     constexpr int KT = T::KT, KSTEPS = D / 16, DT = D / 32, VALU = 0x2, MFMA = 0x8, DS_READ = 0x100;
     __shared__ __align__(1024) unsigned char lds[2][2][T::BYTES];  // [buffer][K, V]
@@ -92,7 +92,8 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
     id /= a.splits;
     const int kv_head = (int)(id % a.kv.kv_heads);
     id /= a.kv.kv_heads;
-    const int b = (int)(id % a.kv.batch), rb = row_blocks - 1 - (int)(id / a.kv.batch);  // the longest rows first
+    int b, rb;
+    if (!a.block_of<T::BM>((int)id, b, rb)) return;
     const int len = a.kv.length(b), fresh = a.new_tokens(b), rows = min(fresh, a.max_q) * a.group;
     const int block0 = rb * T::BM;
     if (block0 >= rows) return;
@@ -436,11 +437,10 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a, int row_b
 }
 
 int launch_attn_tile(const AttnCall &a, int D, hipStream_t st) {
-    const int row_blocks = (int)ceil_div((int64_t)a.max_q * a.group, ATTN_TILE_ROWS);
-    const dim3 grid((unsigned)((int64_t)a.splits * a.kv.kv_heads * row_blocks * a.kv.batch)), block(256);
+    const dim3 grid((unsigned)((int64_t)a.splits * a.kv.kv_heads * a.row_blocks * (a.by_rows ? 1 : a.kv.batch))), block(256);
     const bool aligned = a.kv.page_size % 16 == 0 && a.kv.page_bytes < (1ll << 32) && a.kv.page_size * a.kv.slot_bytes < (1ll << 32);
-    if (D == 128) aligned ? attn_tile_kernel<128, true><<<grid, block, 0, st>>>(a, row_blocks) : attn_tile_kernel<128, false><<<grid, block, 0, st>>>(a, row_blocks);
-    else aligned ? attn_tile_kernel<64, true><<<grid, block, 0, st>>>(a, row_blocks) : attn_tile_kernel<64, false><<<grid, block, 0, st>>>(a, row_blocks);
+    if (D == 128) aligned ? attn_tile_kernel<128, true><<<grid, block, 0, st>>>(a) : attn_tile_kernel<128, false><<<grid, block, 0, st>>>(a);
+    else aligned ? attn_tile_kernel<64, true><<<grid, block, 0, st>>>(a) : attn_tile_kernel<64, false><<<grid, block, 0, st>>>(a);
     const int rc = launch_status();
     return rc == C2R_OK && a.splits > 1 ? launch_attn_join(a, true, D, st) : rc;
 }

@@ -23,21 +23,10 @@ namespace c2r {
 // 37.8, 40.1, 56.5; pairs of neighbours 31.0, 29.5, 36.6.  Below: 2000 tokens of 16/16 19.0 and 19.8, 2005 of 32/8 18.6 and 20.1.
 constexpr int ROPE_TOKENS = 2, ROPE_MANY = 8192;
 
-// The sequence that row t belongs to, or -1 past the last one: how many of q_start[0 .. batch] are at most t, 64 at a time.
+// The sequence that row t belongs to, or -1 past the last one: how many of q_start[0 .. batch] are at most t.
 __device__ __forceinline__ int sequence_of(const int32_t *q_start, int batch, int64_t t) {
-    // (non-decreasing: the wave looks at 64 evenly spread entries, then at the 64 steps between two of them, ...)
-    int lo = 0, n = batch + 1;  // the answer's count lies in lo .. lo + n
-    const int lane = lane_id();
-    while (n > 0) {
-        const int step = (n + 63) / 64, at = lo + (lane + 1) * step - 1;  // last entry of each of 64 runs
-        const bool below = at < lo + n && q_start[at] <= t;
-        const int runs = __popcll(__ballot(below));
-        lo += runs * step;
-        const int rest = n - runs * step;
-        n = rest < step - 1 ? rest : step - 1;
-        if (step == 1) break;
-    }
-    return lo > batch ? -1 : lo - 1;
+    const int n = count_first(batch + 1, [&](int i) { return q_start[i] <= t; });
+    return n > batch ? -1 : n - 1;
 }
 
 // The sum over the LH neighbouring lanes of a head, in each of them.

@@ -372,6 +372,52 @@ def test_prefill_rows_past_the_stated_most_are_untouched(c2r, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("group", [1, 3, 8])
+@pytest.mark.parametrize("chunks", [{0: 300}, {69: 300}, {5: 129, 40: 7, 41: 200}, {30: 128, 31: 0, 32: 0, 33: 256}, {}])
+def test_prefill_of_a_mixed_batch(c2r, dtype, group, chunks):
+    """A few chunks among single tokens and sequences with nothing new, some rows of no sequence before and behind, one chunk with
+    more rows than the stated most."""
+    rng = np.random.default_rng(41 + group + len(chunks))
+    B, before, behind = 70, 5, 4
+    new = [chunks.get(b, 0 if b % 7 == 3 else 1) for b in range(B)]
+    lens = [n + int(rng.integers(0, 200)) for n in new]
+    bt = Batch(c2r, rng, dtype, 64, 2, 16, lens, new)
+    T = before + bt.T + behind
+    q = _randn(rng, T, 2 * group, 64, dtype=dtype)
+    start = bt.q_start + before
+    for most in (max(new), 250):
+        out = torch.full_like(q, 7.0)
+        c2r.attention_prefill(q, bt.cache, start, most, window=90, sinks=3, out=out)
+        here = torch.cat([torch.arange(s, s + min(n, most)) for s, n in zip((bt.q_start + before).tolist(), new)])
+        rest = torch.ones(T, dtype=torch.bool)
+        rest[here] = False
+        assert (out[rest.cuda()] == 7).all()
+
+        class View:
+            pass
+        v = View()
+        v.D, v.rows = 64, bt.rows
+        if most >= max(new):
+            v.new, v.lens = new, lens
+            _check_attention(out[before:before + bt.T], q[before:before + bt.T], v, dtype, 64 ** -0.5, 90, 3)
+        else:       # (a chunk's rows past the most are left out: its first ones stand where they stood)
+            v.new, v.lens = [min(n, most) for n in new], [L - n + min(n, most) for n, L in zip(new, lens)]
+            _check_attention(out[here.cuda()], q[here.cuda()], v, dtype, 64 ** -0.5, 90, 3)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [0.0, -0.2])
+def test_scales_that_are_not_positive(c2r, dtype, scale):
+    rng = np.random.default_rng(42)
+    bt = Batch(c2r, rng, dtype, 128, 1, 16, [150], [70])
+    q = _randn(rng, 70, 2, 128, dtype=dtype)
+    _check_attention(c2r.attention_prefill(q, bt.cache, bt.q_start, 70, scale), q, bt, dtype, scale, 0, 0)
+    bt.new = [1]
+    last = q[-1:].contiguous()
+    _check_attention(c2r.attention_decode(last, bt.cache, scale), last, bt, dtype, scale, 0, 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("T", [8, 9000, 40000, 70000])
 def test_prefill_with_many_rows_of_no_sequence(c2r, dtype, T):
     """Rows that are there for a larger batch: the workspace that is asked for holds the keys' parts, however many rows there are."""
