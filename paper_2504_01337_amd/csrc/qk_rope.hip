@@ -20,7 +20,7 @@ namespace c2r {
 // Waves of one token and of ROPE_TOKENS tokens: a launch that would have ROPE_MANY waves or more at a token each, all heads of
 // the token in one wave (four groups of heads), takes the second.  us with one, two and four tokens a wave (bf16, D 128): 8192
 // tokens of 16/16 heads 49.2, 43.0, 44.2, without a cache 30.6, 26.7, 28.2; 16000 of 32/4 heads 80.6, 69.2, 67.5; 4096 of 32/32
-// 37.8, 40.1, 56.5; pairs of neighbours 31.0, 29.5, 36.6.  Below: 2000 tokens of 16/16 19.0 and 19.8, 2005 of 32/8 18.6 and 20.1.
+// 37.8, 40.1, 56.5; pairs of neighbours 31.0, 29.5, 36.6.  Below: 2000 tokens of 16/16 19.0 and 19.8, 1301 of 32/8, half of a head turned, 14.1 and 18.1.
 constexpr int ROPE_TOKENS = 2, ROPE_MANY = 8192;
 
 // The sequence that row t belongs to, or -1 past the last one: how many of q_start[0 .. batch] are at most t.
@@ -47,17 +47,16 @@ __device__ __forceinline__ float head_sum(float v) {
 
 // TOKENS: tokens in a row that a wave takes.  Their places are looked up side by side, a lane each: the chain of loads behind a
 // place (sequence, length, page) is what a wave that is only just long enough for one token spends its life on.
-// PAIRS: where the two elements of a pair stand in the lanes.  NEAR (neighbours): one lane.  FAR (halves, the whole head turned):
-// one lane too, which then holds 8 bytes of each half.  PART (halves of a part of the head): a lane has 16 bytes in a row, and
-// its partners' come by an exchange; they are normed and their angles worked out twice.  (Whole heads the PART way: 52.3 us for
-// the 8192 tokens with their append, FAR 43.0.)
-enum Pairs { NEAR, FAR, PART };
-template <bool BF16, int D, bool CACHE, Pairs PAIRS, int TOKENS>
+// Both elements of a pair are in one lane: neighbours stand in its 16 bytes; of halves, a lane of the turned part takes 8 bytes
+// of each.  (16 bytes in a row of either and the partners' by an exchange, normed and turned twice: 52.3 us for the 8192 tokens with
+// their append, where this takes 43.0; 1301 tokens, half of a head turned 18.6, 14.1.)
+template <bool BF16, int D, bool CACHE, bool NEIGHBOURS, int TOKENS>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeCall a) {
     constexpr int SZ = BF16 ? 2 : 4, EPL = 16 / SZ, LH = D / EPL, HW = 64 / LH, BATCH = 4;
-    const int lane = lane_id(), sub = lane / LH, c = lane % LH, e0 = c * EPL;
+    const int lane = lane_id(), sub = lane / LH, c = lane % LH;
+    const bool turned = c * EPL < a.rot;
     // this lane's two 8-byte pieces of a row: bytes
-    const int low = PAIRS == FAR ? c * 8 : c * 16, high = PAIRS == FAR ? D * SZ / 2 + c * 8 : low + 8;
+    const int low = !NEIGHBOURS && turned ? c * 8 : c * 16, high = !NEIGHBOURS && turned ? a.rot * SZ / 2 + c * 8 : low + 8;
     const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t run = w / a.parts, first_token = run * TOKENS;
     const int part = (int)(w - run * a.parts);
@@ -74,7 +73,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeCall a) {
             const unsigned char *row = h < a.heads ? a.q + t * a.q_bytes + (int64_t)h * (D * SZ)
                                        : h < a.heads + a.kv_heads ? a.k + t * a.k_bytes + (int64_t)(h - a.heads) * (D * SZ)
                                                                   : a.v + t * a.v_bytes + (int64_t)(h - a.heads - a.kv_heads) * (D * SZ);
-            if constexpr (PAIRS == FAR) {
+            if constexpr (!NEIGHBOURS) {
                 const u32x2 a0 = *reinterpret_cast<const u32x2 *>(row + low), a1 = *reinterpret_cast<const u32x2 *>(row + high);
                 x[u] = u32x4{a0[0], a0[1], a1[0], a1[1]};
             } else {
@@ -83,7 +82,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeCall a) {
         }
     };
     auto store = [&](unsigned char *row, const u32x4 &v) {
-        if constexpr (PAIRS == FAR) {
+        if constexpr (!NEIGHBOURS) {
             *reinterpret_cast<u32x2 *>(row + low) = u32x2{v[0], v[1]};
             *reinterpret_cast<u32x2 *>(row + high) = u32x2{v[2], v[3]};
         } else {
@@ -139,11 +138,8 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeCall a) {
     }
     if (a.position) pos = a.position[mine];
 
-    // weights of this lane's elements and of their partners
-    const int half = a.rot / 2, hl = half / EPL;
-    const bool turned = e0 < a.rot;  // (FAR: all are)
-    const int partner = PAIRS != PART || !turned ? c : c < hl ? c + hl : c - hl;
-    float wq[EPL], wk[EPL], wq_other[EPL], wk_other[EPL];
+    // weights of this lane's elements
+    float wq[EPL], wk[EPL];
     auto weights = [&](const float *src, int first, int second, float (&f)[EPL]) {
 #pragma unroll
         for (int i = 0; i < EPL; i += EPL / 2)
@@ -155,16 +151,11 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeCall a) {
     };
     weights(a.q_weight, low / SZ, high / SZ, wq);
     weights(a.k_weight, low / SZ, high / SZ, wk);
-    if constexpr (PAIRS == PART) {
-        weights(a.q_weight, partner * EPL, partner * EPL + EPL / 2, wq_other);
-        weights(a.k_weight, partner * EPL, partner * EPL + EPL / 2, wk_other);
-    }
     // frequencies of this lane's pairs
-    constexpr int NA = PAIRS == PART ? EPL : EPL / 2;
+    constexpr int NA = EPL / 2;
     float freq[NA];
-    const int f0 = PAIRS == PART ? (c < hl ? e0 : e0 - half) : c * (EPL / 2);
 #pragma unroll
-    for (int i = 0; i < NA; ++i) freq[i] = turned ? a.inv_freq[f0 + i] : 0.0f;
+    for (int i = 0; i < NA; ++i) freq[i] = turned ? a.inv_freq[c * NA + i] : 0.0f;
     auto unpack = [](const u32x4 &v, float (&f)[EPL]) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -193,7 +184,6 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeCall a) {
             cs[k] = __builtin_amdgcn_cosf(r);
             sn[k] = __builtin_amdgcn_sinf(r);
 #endif
-            if (PAIRS == PART && c < hl) sn[k] = -sn[k];  // y_i cos - y_j sin; y_j cos + y_i sin
         }
         for (int first = part; first < groups; first += BATCH * a.parts) {
             u32x4 now[BATCH];
@@ -209,14 +199,8 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeCall a) {
                 if (hg >= groups) break;
                 const int h = hg * HW + sub;
                 const bool is_q = h < a.heads, is_v = h >= a.heads + a.kv_heads, real = h < total;
-                float y[EPL], other[EPL];
+                float y[EPL];
                 unpack(now[u], y);
-                if constexpr (PAIRS == PART) {
-                    u32x4 px;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) px[k] = __shfl(now[u][k], sub * LH + partner);
-                    unpack(px, other);
-                }
                 float sq = 0.0f;
 #pragma unroll
                 for (int k = 0; k < EPL; ++k) sq = __builtin_fmaf(y[k], y[k], sq);
@@ -226,21 +210,13 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeCall a) {
                 if (is_q ? a.q_weight != nullptr : a.k_weight != nullptr) rs = __builtin_amdgcn_rsqf(__builtin_fmaf(sq, 1.0f / D, a.eps));
 #endif
 #pragma unroll
-                for (int k = 0; k < EPL; ++k) {
-                    y[k] = y[k] * rs * (is_q ? wq[k] : wk[k]);
-                    if constexpr (PAIRS == PART) other[k] = other[k] * rs * (is_q ? wq_other[k] : wk_other[k]);
-                }
+                for (int k = 0; k < EPL; ++k) y[k] = y[k] * rs * (is_q ? wq[k] : wk[k]);
                 float out[EPL];
-                if constexpr (PAIRS != PART) {
 #pragma unroll
-                    for (int k = 0; k < EPL / 2; ++k) {
-                        const int i0 = PAIRS == NEAR ? 2 * k : k, i1 = PAIRS == NEAR ? 2 * k + 1 : k + EPL / 2;
-                        out[i0] = y[i0] * cs[k] - y[i1] * sn[k];
-                        out[i1] = y[i1] * cs[k] + y[i0] * sn[k];
-                    }
-                } else {
-#pragma unroll
-                    for (int k = 0; k < EPL; ++k) out[k] = turned ? y[k] * cs[k] + other[k] * sn[k] : y[k];
+                for (int k = 0; k < NA; ++k) {
+                    const int i = NEIGHBOURS ? 2 * k : k, j = NEIGHBOURS ? 2 * k + 1 : k + NA;
+                    out[i] = turned ? y[i] * cs[k] - y[j] * sn[k] : y[i];
+                    out[j] = turned ? y[j] * cs[k] + y[i] * sn[k] : y[j];
                 }
                 u32x4 r;
 #pragma unroll
@@ -260,17 +236,16 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeCall a) {
     }
 }
 
-template <bool BF16, int D, bool CACHE, Pairs PAIRS>
+template <bool BF16, int D, bool CACHE, bool NEIGHBOURS>
 static void start(const RopeCall &a, int tokens, unsigned blocks, hipStream_t st) {
-    if (tokens == 1) qk_norm_rope_kernel<BF16, D, CACHE, PAIRS, 1><<<dim3(blocks), dim3(256), 0, st>>>(a);
-    else qk_norm_rope_kernel<BF16, D, CACHE, PAIRS, ROPE_TOKENS><<<dim3(blocks), dim3(256), 0, st>>>(a);
+    if (tokens == 1) qk_norm_rope_kernel<BF16, D, CACHE, NEIGHBOURS, 1><<<dim3(blocks), dim3(256), 0, st>>>(a);
+    else qk_norm_rope_kernel<BF16, D, CACHE, NEIGHBOURS, ROPE_TOKENS><<<dim3(blocks), dim3(256), 0, st>>>(a);
 }
 
 template <bool BF16, int D, bool CACHE>
 static void start(const RopeCall &a, bool neighbours, int tokens, unsigned blocks, hipStream_t st) {
-    if (neighbours) start<BF16, D, CACHE, NEAR>(a, tokens, blocks, st);
-    else if (a.rot == D) start<BF16, D, CACHE, FAR>(a, tokens, blocks, st);
-    else start<BF16, D, CACHE, PART>(a, tokens, blocks, st);
+    if (neighbours) start<BF16, D, CACHE, true>(a, tokens, blocks, st);
+    else start<BF16, D, CACHE, false>(a, tokens, blocks, st);
 }
 
 int launch_qk_norm_rope(RopeCall a, bool bf16, int D, bool neighbours, hipStream_t st) {
