@@ -489,8 +489,8 @@ int c2r_qk_norm_rope_append(const void *q, int64_t q_stride, const void *k, int6
  *     0 <= j <= p and (window == 0 or j > p - window or j < sinks)
  * key head h / (heads / kv_heads).  window: the last keys that stay visible, 0: all; sinks: first tokens that stay visible
  * beside a window.  A sequence without a visible key (kv_len 0) gets zeros.  What is hidden has no part in the result, an
- * infinity or a NaN there included.  Scores, softmax and sums in 32 bits (bf16: the products' weights are rounded to bf16),
- * rounded once.  Long caches are split over the GPU and joined, with the same bits on every run.
+ * infinity or a NaN there included.  Scores, softmax and sums in 32 bits (bf16: the products' weights keep 16 of them), rounded
+ * once.  Long caches are split over the GPU and joined, with the same bits on every run.
  * q, out     : [batch, heads, head_dim] of the cache's dtype, strides as in c2r_qk_norm_rope
  * max_kv_len : host; the longest kv_len of the batch (0: not known).  It only steers the split: results hold for any value.
  * ws         : c2r_workspace_bytes(C2R_STAGE_ATTENTION, batch, head_dim, heads, kv_heads, 0, dtype) bytes, 256-aligned
@@ -507,7 +507,7 @@ int c2r_attention_decode(const void *q, int64_t q_stride, int heads, const c2r_k
  * max_q_len  : host; at least the most new tokens of a sequence: rows past that many are untouched.  The workspace query
  *              covers T up to batch * max_q_len
  * ws         : c2r_workspace_bytes(C2R_STAGE_ATTENTION, T, head_dim, heads, kv_heads, max_q_len, dtype) bytes, 256-aligned
- * Everything else as c2r_attention_decode.
+ * Everything else as c2r_attention_decode, but bf16's weights are rounded to bf16 on their way to the second product.
  */
 int c2r_attention_prefill(const void *q, int64_t q_stride, int64_t T, int heads, const int32_t *q_start, int64_t max_q_len,
                           const c2r_kv_cache *cache, int64_t max_kv_len, float scale, int64_t window, int64_t sinks, void *out,

@@ -138,9 +138,14 @@ struct Stream {
     __device__ static __forceinline__ void add_values(const Tile &t, const float (&w)[VKEYS], State &st) {
 #if defined(__HIP_DEVICE_COMPILE__)
         if constexpr (BF16) {
-            // the weights are rounded to bf16 for the matrix pipe (the denominator adds them unrounded): a relative 2^-8
-            // at most each, at random, against the 2^-8 of the output's own rounding
-            const u32x4 pw = {pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]), pack_bf16x2(w[6], w[7])};
+            // the matrix pipe takes the weights in two bf16 pieces, the rounded weight and what is left of it: 2^-16 of each at most is
+            // lost, far below the output's own rounding (2^-8), and this kernel's memory-bound loop has the time for both products
+            u32x4 pw, rest;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                pw[c] = pack_bf16x2(w[2 * c], w[2 * c + 1]);
+                rest[c] = pack_bf16x2(w[2 * c] - __uint_as_float(pw[c] << 16), w[2 * c + 1] - __uint_as_float(pw[c] & 0xffff0000u));
+            }
 #pragma unroll
             for (int i = 0; i < VEL; ++i) {
                 const uint32_t sel = i & 1 ? 0x07060302u : 0x05040100u;
@@ -148,6 +153,7 @@ struct Stream {
 #pragma unroll
                 for (int c = 0; c < 4; ++c) vt[c] = __builtin_amdgcn_perm(t.v[2 * c + 1][i >> 1], t.v[2 * c][i >> 1], sel);
                 st.o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt), __builtin_bit_cast(bf16x8, pw), st.o[i], 0, 0, 0);
+                st.o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt), __builtin_bit_cast(bf16x8, rest), st.o[i], 0, 0, 0);
             }
         } else {
 #pragma unroll

@@ -1,0 +1,41 @@
+"""Attention, norms and the cache where they are easiest to get wrong: roundings, keys in parts, kernels behind a size threshold,
+lengths past the cache, scales of either sign.  Against the definitions in 64 bits (oracle/attention.py); the tolerances' terms are those
+of test_gpu_attention.py."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import attention as oa
+from test_gpu_attention import B8, U, Batch, _np, _randn
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def c2r():
+    from paper_2504_01337_amd import c2r as m
+    m.lib()
+    return m
+
+
+def _sums(D, n, size, spread):
+    """What 32-bit scores, weights and sums over n keys may be off."""
+    return (2 * (D + 4) * spread + 2 * max(n, 1) + 16) * U * size + 1e-37
+
+
+# ---- roundings ----
+
+@pytest.mark.parametrize("D,H,Hkv,lens,window,sinks", [
+    (128, 2, 2, [1, 2, 17, 300], 0, 0), (64, 8, 1, [1000, 33], 0, 0), (128, 20, 1, [4000], 0, 0), (64, 3, 3, [600, 2000], 130, 5)])
+def test_decode_rounds_the_result_alone(c2r, D, H, Hkv, lens, window, sinks):
+    """bf16: the weights reach the matrix pipe in two pieces, which leaves 2^-16 of each; the result's rounding is 2^-8 of it."""
+    rng = np.random.default_rng(51 + D + H)
+    bt = Batch(c2r, rng, "bf16", D, Hkv, 16, lens)
+    q = _randn(rng, len(lens), H, D, dtype="bf16")
+    got = _np(c2r.attention_decode(q, bt.cache, None, window, sinks, max(lens)))
+    for b, n in enumerate(lens):
+        k, v = (_np(x) for x in bt.rows[b])
+        ref, size, spread = oa.attention(_np(q[b:b + 1]), k, v, n - 1, D ** -0.5, window, sinks)
+        tol = _sums(D, n, size, spread) + 2.0 ** -16 * size + B8 * np.abs(ref)
+        err = np.abs(got[b:b + 1] - ref)
+        assert (err <= tol).all(), (b, float((err / tol).max()))
