@@ -78,6 +78,15 @@ __device__ __forceinline__ float add_halves(float v) {
     return v;
 }
 
+// v + both of a pair of bf16 numbers
+__device__ __forceinline__ float add_pair(float v, uint32_t pair) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    v = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), bf16x2{(__bf16)1.0f, (__bf16)1.0f}, v, false);
+#endif
+    return v;
+}
+
 // ALIGNED: pages of whole groups of 16 keys, and of less than 4 GB, so that the 16 rows which a wave copies of a tile lie in
 // one page: one look-up and one scalar address.  Working out every lane's page takes as many vector instructions per tile as
 // the softmax.
@@ -256,15 +265,18 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a) {
             for (int e = 1; e < 16; ++e) top = fmaxf(top, s[u][e]);
             return top;
         };
-        // weights rounded to bf16 for the matrix pipe, added unrounded
+        // Weights are rounded to bf16 for the matrix pipe, 2^-8 of each, and added up as rounded (v_dot2c_f32_bf16, both of a pair in one
+        // instruction): a row that sees one key is its value exactly.  A second product with what the rounding leaves would give the
+        // 32-bit weights' result and costs a quarter to a third: 4 x 2048 tokens 85 us and 109, one prompt of 8192 288 and 383, root mean
+        // square error 2.2e-3 and 1.6e-3, of which the result's own rounding is 1.6e-3.
         auto weigh = [&](int u) {
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
                 const float lo = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], a.scale_log2, -m));
                 const float hi = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e + 1], a.scale_log2, -m));
-                l += lo;
-                l += hi;
-                w[u][e >> 3][(e >> 1) & 3] = pack_bf16x2(lo, hi);
+                const uint32_t pair = pack_bf16x2(lo, hi);
+                w[u][e >> 3][(e >> 1) & 3] = pair;
+                l = add_pair(l, pair);
             }
         };
 #if defined(__HIP_DEVICE_COMPILE__)

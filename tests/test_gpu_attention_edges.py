@@ -39,3 +39,17 @@ def test_decode_rounds_the_result_alone(c2r, D, H, Hkv, lens, window, sinks):
         tol = _sums(D, n, size, spread) + 2.0 ** -16 * size + B8 * np.abs(ref)
         err = np.abs(got[b:b + 1] - ref)
         assert (err <= tol).all(), (b, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("page", [1, 16])
+@pytest.mark.parametrize("D,H,Hkv", [(128, 2, 2), (64, 6, 2)])
+def test_one_visible_key_is_its_value(c2r, D, H, Hkv, page):
+    """bf16, a window of 1: whatever the weight is rounded to, it is its own denominator."""
+    rng = np.random.default_rng(52 + D + page)
+    new, lens = [150, 1, 40], [150, 9, 400]
+    bt = Batch(c2r, rng, "bf16", D, Hkv, page, lens, new)
+    q = _randn(rng, bt.T, H, D, dtype="bf16")
+    want = torch.cat([v[n - m:] for (_, v), n, m in zip(bt.rows, lens, new)]).repeat_interleave(H // Hkv, 1)
+    assert torch.equal(c2r.attention_prefill(q, bt.cache, bt.q_start, max(new), window=1), want)
+    last = (bt.q_start[1:] - 1).long()
+    assert torch.equal(c2r.attention_decode(q[last], bt.cache, window=1), want[last])
