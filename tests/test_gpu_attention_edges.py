@@ -53,3 +53,22 @@ def test_one_visible_key_is_its_value(c2r, D, H, Hkv, page):
     assert torch.equal(c2r.attention_prefill(q, bt.cache, bt.q_start, max(new), window=1), want)
     last = (bt.q_start[1:] - 1).long()
     assert torch.equal(c2r.attention_decode(q[last], bt.cache, window=1), want[last])
+
+
+@pytest.mark.parametrize("D,nb", [(64, False), (128, True)])
+def test_sine_and_cosine_in_full_precision(c2r, D, nb):
+    """fp32, pairs (1, 0), which turn into (cos, sin).  Of an angle of pi/4 at most: its rounding 0.35 u of the result, the result's 0.5 u,
+    those of the square and of the series 0.4 u at most: 1.5 u."""
+    from test_gpu_attention import _freq
+    rng = np.random.default_rng(53 + D)
+    T = 3000
+    q = torch.zeros((T, 1, D), device="cuda")
+    if nb:
+        q[..., ::2] = 1.0
+    else:
+        q[..., :D // 2] = 1.0
+    pos = rng.integers(0, 1 << 17, T).astype(np.int32)
+    f = _freq(D)
+    got = c2r.qk_norm_rope(q, q, f, torch.from_numpy(pos).cuda(), neighbours=nb)[0]
+    ref, _ = oa.norm_rope(_np(q), None, 0.0, f.cpu().numpy(), pos, nb)
+    assert np.abs(_np(got) - ref).max() <= 1.5 * U, np.abs(_np(got) - ref).max() / U
