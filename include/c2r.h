@@ -440,7 +440,8 @@ int c2r_distinct_devices(const int32_t *topk_idx, int64_t T, int K, int E, const
  * so both [page][head][slot][element] and [page][slot][head][element] are cache layouts, and one page per sequence is a
  * dense cache.  page_size is any number from 1 on.  kv_len[b] counts the tokens of sequence b that the cache holds, the new
  * ones of this step included.  page_table int32[batch, max_pages] and kv_len int32[batch] live in DEVICE memory.
- * Lengths are cut to [0, max_pages * page_size]; a page number outside [0, n_pages) (a page given back, say) is never
+ * A negative kv_len is 0.  One past max_pages * page_size counts tokens that have no place: positions count them (up to 2^30), they are
+ * not stored, and no query sees them; what is cached stays as it is.  A page number outside [0, n_pages) (a page given back, say) is never
  * written and reads as page 0, which matters only if a query sees a key of it.
  * Limits (else C2R_ERR_UNSUPPORTED): head_dim 64 or 128; up to 1024 heads; batch, pages and tokens below 2^30, page_size *
  * max_pages below 2^28, batch * heads of a decoding step below 2^24.  C2R_ERR_INVALID_ARG: query heads not a multiple of kv_heads, rows or strides that are not whole 16-byte
@@ -476,7 +477,7 @@ int c2r_qk_norm_rope(const void *q, int64_t q_stride, const void *k, int64_t k_s
  * take the last places of its kv_len[b]; q_start == NULL: one token per sequence (T == batch).
  * q_start  : int32[batch + 1] in DEVICE memory, non-decreasing; rows of no sequence are left out, their q_out untouched
  * position : int32[T], or NULL: the token's place in the cache
- * A token whose place is below 0 (kv_len smaller than the new tokens) is rotated and not stored.
+ * A token whose place is below 0 (kv_len smaller than the new tokens) or past the table's end is rotated and not stored.
  */
 int c2r_qk_norm_rope_append(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride, int64_t T,
                             int heads, const float *q_weight, const float *k_weight, float eps, const float *inv_freq, int rot_dim,
@@ -486,9 +487,9 @@ int c2r_qk_norm_rope_append(const void *q, int64_t q_stride, const void *k, int6
 /*
  * Attention of one new token per sequence over the cache (a decoding step of the decoder blocks of Sec. 4.1's models):
  *     out[b, h] = sum_j softmax_j(scale * q[b, h] . k_j) v_j   over the keys j that the token at p = kv_len[b] - 1 sees:
- *     0 <= j <= p and (window == 0 or j > p - window or j < sinks)
+ *     0 <= j <= p, j < max_pages * page_size, and (window == 0 or j > p - window or j < sinks)
  * key head h / (heads / kv_heads).  window: the last keys that stay visible, 0: all; sinks: first tokens that stay visible
- * beside a window.  A sequence without a visible key (kv_len 0) gets zeros.  What is hidden has no part in the result, an
+ * beside a window.  A sequence without a visible key (kv_len 0, say) gets zeros.  What is hidden has no part in the result, an
  * infinity or a NaN there included.  Scores, softmax and sums in 32 bits (bf16: the products' weights keep 16 of them), rounded
  * once.  Long caches are split over the GPU and joined, with the same bits on every run.
  * q, out     : [batch, heads, head_dim] of the cache's dtype, strides as in c2r_qk_norm_rope

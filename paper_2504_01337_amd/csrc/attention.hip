@@ -53,6 +53,7 @@ static KvView view_of(const c2r_kv_cache &c) {
     v.page_size = (int32_t)c.page_size;
     v.max_pages = (int32_t)c.max_pages;
     v.batch = (int32_t)c.batch;
+    v.capacity = (int32_t)(c.page_size * c.max_pages);
     v.kv_heads = (int32_t)c.kv_heads;
     // j / d for j < 2^31: s = ceil(log2 d), mul = floor(2^32 (2^s - d) / d) + 1
     uint32_t s = 0;
@@ -162,8 +163,8 @@ static int attention_call(const void *q, int64_t q_stride, int64_t T, int heads,
     a.T = T;
     a.max_q = 1;
     a.heads = heads, a.group = heads / (int)cache->kv_heads;
-    // a window that holds whole sequences is none, and more sinks than keys are all of them
-    a.window = window >= capacity ? 0 : (int)window;
+    // a window of as many tokens as a sequence can have is none, and more sinks than keys are all of them
+    a.window = window >= ATTN_MOST ? 0 : (int)window;
     a.sinks = a.window == 0 ? 0 : sinks > capacity ? (int)capacity : (int)sinks;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.splits = 1;
@@ -187,7 +188,7 @@ static int64_t prompt_parts(const AttnCall &a, int64_t blocks, int64_t tiles, in
     // (a batch's T rows may be far fewer than batch * max_q; every sequence and key head has a block that is not full)
     const double rows = (double)a.T * a.heads, real = rows / ATTN_TILE_ROWS + a.kv.batch * a.kv.kv_heads * 0.5;
     const double units = real < blocks ? real : blocks, rate = D == 128 ? 1.6 : 0.92;
-    const double fewest = a.window ? 0.9 * tiles : a.max_q < longest ? tiles * (1.0 - (double)a.max_q / longest) : 0.0;
+    const double fewest = a.window && a.window < a.kv.capacity ? 0.9 * tiles : a.max_q < longest ? tiles * (1.0 - (double)a.max_q / longest) : 0.0;
     constexpr int SAMPLES = 8;
     int64_t best = 1;
     double least = 0.0;

@@ -18,16 +18,13 @@ struct KvView {
     int64_t page_bytes, slot_bytes, head_bytes;
     const int32_t *table, *kv_len;
     int32_t n_pages, page_size, max_pages, batch, kv_heads;
+    int32_t capacity;  // keys that a sequence's row of the table can name
     uint32_t div_mul, div_shift;  // key index / page_size = (mulhi(div_mul, j) + j) >> div_shift, j < 2^31
 
     __device__ __forceinline__ int page_of(int j) const { return (int)((__umulhi(div_mul, (uint32_t)j) + (uint32_t)j) >> div_shift); }
-    // Cached tokens of sequence b, never more than its row of the table can name.
-    __device__ __forceinline__ int length(int b) const {
-        const int64_t most = (int64_t)max_pages * page_size;
-        const int n = kv_len[b];
-        return n < 0 ? 0 : (int64_t)n > most ? (int)most : n;
-    }
-    // The table's entry for key j of sequence b (j below length(b)), as it stands there: nothing waits for it before it is used.
+    // Tokens of sequence b.  Those from place `capacity` on are in no page: positions count them, and no query sees them.
+    __device__ __forceinline__ int tokens(int b) const { return min(max(kv_len[b], 0), 1 << 30); }
+    // The table's entry for key j of sequence b (j below capacity), as it stands there: nothing waits for it before it is used.
     __device__ __forceinline__ int page(int b, int j) const { return table[(int64_t)b * max_pages + page_of(j)]; }
     // Where key j lies; an entry outside the cache reads as page 0.
     __device__ __forceinline__ int64_t offset(int page, int j) const {
@@ -101,8 +98,11 @@ struct AttnCall {
         rb = (int)((rows + BM - 1) / BM) - 1 - (x - begin(b));
         return rb >= 0;
     }
-    // Whether the query at position p sees key j.
-    __device__ __forceinline__ bool sees(int p, int j) const { return j <= p && (!window || j > p - window || j < sinks); }
+    // The last key that is cached of those up to position p.
+    __device__ __forceinline__ int last_key(int p) const { return min(p, kv.capacity - 1); }
+    // Whether the query at position p sees key j; whether it sees none.
+    __device__ __forceinline__ bool sees(int p, int j) const { return j <= last_key(p) && (!window || j > p - window || j < sinks); }
+    __device__ __forceinline__ bool blind(int p) const { return p < 0 || (window && !sinks && p - window >= kv.capacity - 1); }
 };
 
 // The key tiles (KT keys, aligned) that queries at positions p_min .. p_max look at: those of the first `sinks` keys that lie
@@ -118,7 +118,8 @@ struct KeyTiles {
             const int s = (int)(((int64_t)a.sinks + KT - 1) / KT);
             sink_tiles = s < first ? s : first;
         }
-        count = p_max < 0 ? 0 : sink_tiles + p_max / KT - first + 1;
+        const int last = a.last_key(p_max);  // (a window that begins past the cache's end leaves the sinks)
+        count = last < 0 ? 0 : sink_tiles + max(last / KT - first + 1, 0);
     }
     __device__ __forceinline__ int base(int x) const { return (x < sink_tiles ? x : first + x - sink_tiles) * KT; }
     // [x0, x1): the part of split s.  The last one takes what is left, however long a sequence is.
@@ -134,7 +135,7 @@ struct KeyTiles {
 // A tile [base, base + KT) that every query of p_min .. p_max sees whole.
 template <int KT>
 __device__ __forceinline__ bool tile_whole(const AttnCall &a, int base, int p_min, int p_max) {
-    return base + KT - 1 <= p_min && (!a.window || base > p_max - a.window || base + KT <= a.sinks);
+    return base + KT - 1 <= a.last_key(p_min) && (!a.window || base > p_max - a.window || base + KT <= a.sinks);
 }
 
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }

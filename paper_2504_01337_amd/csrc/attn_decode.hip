@@ -18,7 +18,7 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void attn_decode_kernel(Attn
     const uint32_t col_sets = (a.group + 15) / 16, sets = a.kv.kv_heads * col_sets;
     const uint32_t id = blockIdx.x / a.splits, split = blockIdx.x - id * a.splits, b = id / sets, set = id - b * sets;
     const int kv_head = (int)(set / col_sets), col0 = (int)(set - kv_head * col_sets) * 16, left = min(a.group - col0, 16);
-    const int p = a.kv.length(b) - 1, head0 = kv_head * a.group + col0;
+    const int p = a.kv.tokens(b) - 1, head0 = kv_head * a.group + col0;
     const KeyTiles<KT> tiles(a, p, p);
     int x0, x1;
     tiles.part(a, split, x0, x1);
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void attn_decode_kernel(Attn
             for (int e = 0; e < 4; ++e) sum[e] = __builtin_fmaf(f, o[e], sum[e]);
         }
         if (uncut) {
-            const float inv = p < 0 ? 0.0f : 1.0f / l, v[4] = {sum[0] * inv, sum[1] * inv, sum[2] * inv, sum[3] * inv};
+            const float inv = a.blind(p) ? 0.0f : 1.0f / l, v[4] = {sum[0] * inv, sum[1] * inv, sum[2] * inv, sum[3] * inv};
             store_elements<BF16, 4>(a.out + b * a.out_bytes + ((int64_t)(head0 + col) * D + d) * SZ, v);
         } else {
             *reinterpret_cast<f32x4 *>(a.part_o + (part_row + col) * D + d) = sum;

@@ -21,7 +21,7 @@ __global__ __launch_bounds__(256, 3) void attn_rows_kernel(AttnCall a) {
     id /= a.kv.kv_heads;
     int b, rb;
     if (!a.block_of<ATTN_ROWS_ROWS>((int)id, b, rb)) return;
-    const int fresh = a.new_tokens(b), before = a.kv.length(b) - fresh, rows = min(fresh, a.max_q) * a.group;
+    const int fresh = a.new_tokens(b), before = a.kv.tokens(b) - fresh, rows = min(fresh, a.max_q) * a.group;
     const int row0 = (rb * 4 + wave) * 16, left = min(rows - row0, 16);
     if (left <= 0) return;
     // the lane's column: query token ti, head hh of the group; columns past the end repeat the last one
@@ -53,12 +53,12 @@ __global__ __launch_bounds__(256, 3) void attn_rows_kernel(AttnCall a) {
             const float inv = 1.0f / l;
             float *out = reinterpret_cast<float *>(a.out + tok * a.out_bytes + (int64_t)hd * (D * 4)) + at;
 #pragma unroll
-            for (int e = 0; e < N; ++e) out[e] = pos < 0 ? 0.0f : v[e] * inv;
+            for (int e = 0; e < N; ++e) out[e] = a.blind(pos) ? 0.0f : v[e] * inv;
         } else {
             const int64_t pr = (int64_t)split * part_rows + tok * a.heads + hd;
 #pragma unroll
             for (int e = 0; e < N; ++e) a.part_o[pr * D + at + e] = v[e];
-            if (ml) a.part_ml[pr * 2] = m, a.part_ml[pr * 2 + 1] = pos < 0 || x0 == x1 ? PART_EMPTY : l;
+            if (ml) a.part_ml[pr * 2] = m, a.part_ml[pr * 2 + 1] = a.blind(pos) || x0 == x1 ? PART_EMPTY : l;
         }
     };
     if (n < left) {

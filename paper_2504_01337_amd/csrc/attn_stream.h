@@ -169,6 +169,7 @@ struct Stream {
     template <int STEP>
     __device__ static __forceinline__ void run(const AttnCall &a, const u32x4 (&q)[KSTEPS], State &st, const KeyTiles<KT> &tiles, int x0, int x1,
                                                int b, int64_t head_off, int p, int p_min, int p_max) {
+        const int last = a.last_key(p_max);
         // A tile's key registers are free once its scores are there, its value registers once they are added: the next
         // tile's rows are asked for at these two places, so one tile's registers keep a tile's loads in flight all the time.
         // Loads come back in the order they were sent; page numbers are asked for two tiles ahead, for when their rows are
@@ -177,19 +178,19 @@ struct Stream {
         const int count = x0 < x1 ? (x1 - x0 + STEP - 1) / STEP : 0;
         if (count == 0) return;
         auto base = [&](int i) { return tiles.base(x0 + min(i, count - 1) * STEP); };
-        auto pages = [&](int i) { return look_up(a, b, base(i), p_max); };
+        auto pages = [&](int i) { return look_up(a, b, base(i), last); };
         Tile t;
         f32x4 s[SUB];
         float w[VKEYS];
         const int page = pages(0);
         int next = pages(1);
-        const int64_t first = place(a, page, head_off, base(0), p_max);
+        const int64_t first = place(a, page, head_off, base(0), last);
         load_keys(a, t, first);
         load_values(a, t, first);
         for (int i = 0; i + 1 < count; ++i) {
             const int after = pages(i + 2);
             scores(t, q, s);
-            const int64_t at = place(a, next, head_off, base(i + 1), p_max);
+            const int64_t at = place(a, next, head_off, base(i + 1), last);
             load_keys(a, t, at);
             weights(a, s, st, base(i), p, tile_whole<KT>(a, base(i), p_min, p_max), w);
             add_values(t, w, st);

@@ -91,7 +91,7 @@ __device__ __forceinline__ float add_pair(float v, uint32_t pair) {
 // one page: one look-up and one scalar address.  Working out every lane's page takes as many vector instructions per tile as
 // the softmax.
 template <int D, bool ALIGNED>
-__global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a) {
+__global__ __launch_bounds__(256, D == 128 ? 2 : 4) void attn_tile_kernel(AttnCall a) {
     using T = TileShape<D>;
     constexpr int KT = T::KT, KSTEPS = D / 16, DT = D / 32, VALU = 0x2, MFMA = 0x8, DS_READ = 0x100;
     __shared__ __align__(1024) unsigned char lds[2][2][T::BYTES];  // [buffer][K, V]
@@ -103,13 +103,13 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a) {
     id /= a.kv.kv_heads;
     int b, rb;
     if (!a.block_of<T::BM>((int)id, b, rb)) return;
-    const int len = a.kv.length(b), fresh = a.new_tokens(b), rows = min(fresh, a.max_q) * a.group;
+    const int len = a.kv.tokens(b), fresh = a.new_tokens(b), rows = min(fresh, a.max_q) * a.group;
     const int block0 = rb * T::BM;
     if (block0 >= rows) return;
     const int before = len - fresh;
     const int block_rows = min(rows - block0, T::BM);
     // the block's range of positions, and this wave's
-    const int bp_min = before + block0 / a.group, bp_max = before + (block0 + block_rows - 1) / a.group;
+    const int bp_min = before + block0 / a.group, bp_max = before + (block0 + block_rows - 1) / a.group, last = a.last_key(bp_max);
     const int row0 = block0 + wave * 32, left = min(rows - row0, 32);
     const int wr0 = min(row0, rows - 1), wr1 = min(row0 + 31, rows - 1);
     const int p_min = before + wr0 / a.group, p_max = before + wr1 / a.group;
@@ -152,10 +152,10 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a) {
     auto look_up = [&](int x) {
         const int base = tiles.base(x);
         if constexpr (ALIGNED) {
-            pages[0] = a.kv.page(b, min(base + wave * WAVE_ROWS, bp_max));
+            pages[0] = a.kv.page(b, min(base + wave * WAVE_ROWS, last));
         } else {
 #pragma unroll
-            for (int u = 0; u < T::COPIES; ++u) pages[u] = a.kv.page(b, min(base + first_row(u) + lane_row, bp_max));
+            for (int u = 0; u < T::COPIES; ++u) pages[u] = a.kv.page(b, min(base + first_row(u) + lane_row, last));
         }
     };
     const unsigned char *const k_head = a.kv.k + head_off, *const v_head = a.kv.v + head_off;
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a) {
         const int base = tiles.base(x);
         if constexpr (ALIGNED) {
             const uint32_t named = __builtin_amdgcn_readfirstlane(pages[0]), page = named < (uint32_t)a.kv.n_pages ? named : 0;
-            const int j0 = min(base + wave * WAVE_ROWS, bp_max & ~(WAVE_ROWS - 1)), over = bp_max - j0;
+            const int j0 = min(base + wave * WAVE_ROWS, last & ~(WAVE_ROWS - 1)), over = last - j0;
             const uint32_t slot = j0 - a.kv.page_of(j0) * a.kv.page_size;
             const uint64_t at = (uint64_t)page * (uint32_t)a.kv.page_bytes + slot * (uint32_t)a.kv.slot_bytes;
             uint32_t off[T::COPIES];
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a) {
         } else {
 #pragma unroll
             for (int u = from; u < to; ++u) {
-                const int64_t at = a.kv.offset(pages[u], min(base + first_row(u) + lane_row, bp_max)) + piece(u) * 16;
+                const int64_t at = a.kv.offset(pages[u], min(base + first_row(u) + lane_row, last)) + piece(u) * 16;
                 copy16_far(k_head + at, &lds[buf][0][first_row(u) * (D * 2)]);
                 copy16_far(v_head + at, &lds[buf][1][first_row(u) * (D * 2)]);
             }
@@ -252,7 +252,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a) {
             // in keys from this lane's first one on; worked out here and nowhere before (few tiles need it)
             int first = base + u * 32;
             asm volatile("" : "+s"(first));
-            const int at = first + h * 4, to = p - at, from = a.window ? p - a.window - at : -1, sinks = a.window ? a.sinks - at : 0;
+            const int at = first + h * 4, to = a.last_key(p) - at, from = a.window ? p - a.window - at : -1, sinks = a.window ? a.sinks - at : 0;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int c = (e >> 2) * 8 + (e & 3);
@@ -399,7 +399,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a) {
     // ---- results: lane (h, n), word e of o[d]: element 32 d + 8 (e / 4) + 4 h + e % 4 of row n ----
     if (n < left) {
         if (uncut) {
-            const float inv = p < 0 ? 0.0f : 1.0f / l;
+            const float inv = a.blind(p) ? 0.0f : 1.0f / l;
             unsigned char *out = a.out + token * a.out_bytes + (int64_t)head * (D * 2);
 #if defined(__HIP_DEVICE_COMPILE__)
 #pragma unroll
@@ -424,7 +424,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a) {
 #pragma unroll
                 for (int e = 0; e < 16; e += 4)
                     *reinterpret_cast<f32x4 *>(a.part_o + prow * D + d * 32 + e * 2 + h * 4) = f32x4{o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]};
-            if (h == 0) a.part_ml[prow * 2] = m, a.part_ml[prow * 2 + 1] = p < 0 ? PART_EMPTY : l;
+            if (h == 0) a.part_ml[prow * 2] = m, a.part_ml[prow * 2 + 1] = a.blind(p) ? PART_EMPTY : l;
         }
     }
     while (redo) {
@@ -435,7 +435,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a) {
         float me, le, v[D / 64];
         exact_row<true, D, KT>(a, tiles, x0, x1, 1, b, kv_head, before + ic, a.q + tc * a.q_bytes + (int64_t)hc * (D * 2), me, le, v);
         if (uncut) {
-            const float inv = before + ic < 0 ? 0.0f : 1.0f / le;
+            const float inv = a.blind(before + ic) ? 0.0f : 1.0f / le;
             uint16_t *out = reinterpret_cast<uint16_t *>(a.out + tc * a.out_bytes + (int64_t)hc * (D * 2)) + lane * (D / 64);
 #pragma unroll
             for (int e = 0; e < D / 64; ++e) out[e] = (uint16_t)f32_to_bf16_bits(v[e] * inv);
@@ -443,7 +443,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(AttnCall a) {
             const int64_t prow = (int64_t)split * part_rows + tc * a.heads + hc;
 #pragma unroll
             for (int e = 0; e < D / 64; ++e) a.part_o[prow * D + lane * (D / 64) + e] = v[e];
-            if (lane == 0) a.part_ml[prow * 2] = me, a.part_ml[prow * 2 + 1] = before + ic < 0 ? PART_EMPTY : le;
+            if (lane == 0) a.part_ml[prow * 2] = me, a.part_ml[prow * 2 + 1] = a.blind(before + ic) ? PART_EMPTY : le;
         }
     }
 }

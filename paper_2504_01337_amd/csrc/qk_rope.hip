@@ -153,11 +153,11 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeCall a) {
         if (b < 0) {
             place = -2;
         } else if (lane < tokens) {
-            const int len = a.kv.length(b);
+            const int len = max(a.kv.kv_len[b], 0);
             int64_t end = mine + 1;
             if (a.q_start) end = a.q_start[b + 1] < a.T ? a.q_start[b + 1] : a.T;
             pos = len - (int)(end - mine);
-            if (pos >= 0 && pos < len) {
+            if (pos >= 0 && pos < a.kv.capacity) {  // (past the end there is no place, and the tokens before it stay)
                 const int page = a.kv.table[(int64_t)b * a.kv.max_pages + a.kv.page_of(pos)];
                 if ((uint32_t)page < (uint32_t)a.kv.n_pages) place = a.kv.offset(page, pos);
             }

@@ -72,3 +72,62 @@ def test_sine_and_cosine_in_full_precision(c2r, D, nb):
     got = c2r.qk_norm_rope(q, q, f, torch.from_numpy(pos).cuda(), neighbours=nb)[0]
     ref, _ = oa.norm_rope(_np(q), None, 0.0, f.cpu().numpy(), pos, nb)
     assert np.abs(_np(got) - ref).max() <= 1.5 * U, np.abs(_np(got) - ref).max() / U
+
+
+# ---- lengths past the cache ----
+
+def _check(got, q, bt, dtype, window, sinks, weights=0.0):
+    """bt.lens: positions count from there; bt.rows: what is cached."""
+    t, got, qn = 0, _np(got), _np(q)
+    for b, m in enumerate(bt.new):
+        k, v = (_np(x) for x in bt.rows[b])
+        ref, size, spread = oa.attention(qn[t:t + m], k, v, bt.lens[b] - m, bt.D ** -0.5, window, sinks)
+        tol = _sums(bt.D, len(k), size, spread) + (B8 * np.abs(ref) + weights * size if dtype == "bf16" else 0.0)
+        err = np.abs(got[t:t + m] - ref)
+        assert (err <= tol).all(), (b, float((err / tol).max()))
+        t += m
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("most", [64, 2048])                  # keys that a sequence's row of the table can name: 4 pages, 128 pages
+@pytest.mark.parametrize("window,sinks", [(0, 0), (20, 0), (20, 3), (700, 70), (4096, 0)])
+def test_lengths_past_the_cache(c2r, dtype, most, window, sinks):
+    """A chunk of which 5 tokens have no place, a token behind a full cache, one that fills it, one far behind."""
+    rng = np.random.default_rng(54 + most)
+    D, H, Hkv, page = 64, 4, 2, 16
+    new, lens = [12, 1, 1, 3, 7], [most + 5, most + 1, most, most + 5000, 40]
+    held = [min(n, most) for n in lens]
+    bt = Batch(c2r, rng, dtype, D, Hkv, page, held, new, junk=3.0, extra=0)
+    assert bt.table.shape[1] * page == most
+    bt.cache.kv_len.copy_(torch.tensor(lens, dtype=torch.int32))
+    bt.lens = lens
+    q, k, v = (_randn(rng, bt.T, h, D, dtype=dtype) for h in (H, Hkv, Hkv))
+    before_k, before_v = bt.cache.k.clone(), bt.cache.v.clone()
+    place = np.concatenate([np.arange(n - m, n) for n, m in zip(lens, new)]).astype(np.int32)
+    seq = np.repeat(np.arange(5), new)
+    from test_gpu_attention import _check_rope, _freq
+    w, f = _randn(rng, D), _freq(D)
+    got = c2r.qk_norm_rope_append(q, k, v, bt.cache, f, bt.q_start, None, w, w)
+    _check_rope(got, q, w, 1e-6, f, place, False, dtype)
+    ko = c2r.qk_norm_rope(q, k, f, torch.from_numpy(place).cuda(), w, w)[1]
+    for t in range(bt.T):
+        if place[t] < most:
+            p, s, b = int(bt.table[seq[t], place[t] // page]), int(place[t] % page), seq[t]
+            before_k[p, :, s], before_v[p, :, s] = ko[t], v[t]
+            bt.rows[b][0][place[t]], bt.rows[b][1][place[t]] = ko[t], v[t]
+    assert torch.equal(bt.cache.k, before_k) and torch.equal(bt.cache.v, before_v)       # older tokens stay where they are
+    assert sum(place < most) == bt.T - 9
+    for longest in (0, max(lens)):
+        out = c2r.attention_prefill(q, bt.cache, bt.q_start, max(new), None, window, sinks, longest)
+        _check(out, q, bt, dtype, window, sinks, weights=B8)
+    if window == 20 and sinks == 0:
+        assert not out[14:17].any() and out[13].any()         # the one far behind sees nothing; the one that fills the cache does
+    # a token at a time
+    last = (bt.q_start[1:] - 1).long()
+    one = q[last].contiguous()
+    bt.new = [1] * 5
+    for longest in (0, max(lens)):
+        _check(c2r.attention_decode(one, bt.cache, None, window, sinks, longest), one, bt, dtype, window, sinks, weights=2.0 ** -16)
+    kk, vv = k[last].contiguous(), v[last].contiguous()
+    c2r.qk_norm_rope_append(one, kk, vv, bt.cache, f, None, None, w, w)
+    assert torch.equal(bt.cache.k, before_k) and torch.equal(bt.cache.v, before_v)       # they were there, or have no place
