@@ -78,9 +78,25 @@ class Decoder:
         for b in blocks[1:]:
             c = b.cache(batch * per, page_size, batch, per)
             self.caches.append(c2r.PagedKVCache(c.k, c.v, first.page_table, first.kv_len))
+        self.lengths = [0] * batch      # kv_len as the host knows it
+
+    def _grow(self, new):
+        """The lengths with `new` more rows of each sequence; a row past max_len would have no place in the caches."""
+        if len(new) != len(self.lengths) or min(new) < 0:
+            raise ValueError(f"{len(self.lengths)} sequences, new rows {new}")
+        lengths = [n + m for n, m in zip(self.lengths, new)]
+        if max(lengths) > self.max_len:
+            raise ValueError(f"sequence {lengths.index(max(lengths))} would have {max(lengths)} rows, the caches hold {self.max_len}")
+        self.lengths = lengths
+
+    def reset(self):
+        """Empty sequences."""
+        self.kv_len.zero_()
+        self.lengths = [0] * len(self.lengths)
 
     def prompt(self, x, lengths):
         """x[sum(lengths), d]: the next lengths[b] rows of each sequence."""
+        self._grow(lengths)
         new = torch.tensor(lengths, dtype=torch.int32)
         q_start = torch.zeros(len(lengths) + 1, dtype=torch.int32)
         q_start[1:] = new.cumsum(0)
@@ -92,6 +108,7 @@ class Decoder:
 
     def step(self, x):
         """x[batch, d]: the next row of each sequence."""
+        self._grow([1] * len(self.lengths))
         self.kv_len += 1
         for block, cache in zip(self.blocks, self.caches):
             x = block.forward(x, cache, max_kv_len=self.max_len)
@@ -120,7 +137,7 @@ def main():
         torch.cuda.synchronize()
         return y, time.perf_counter() - t
     dec.prompt(x, a.prompts)                    # (first calls load the kernels)
-    dec.kv_len.zero_()
+    dec.reset()
     y, t = timed(dec.prompt, x, a.prompts)
     print(f"{w.name}: {len(x)} rows of {len(a.prompts)} prompts through {a.blocks} blocks: {t * 1e3:.2f} ms")
     last = rms_norm(y[torch.tensor(a.prompts).cumsum(0).cuda() - 1])
