@@ -24,6 +24,8 @@ def rms_norm(x, eps=1e-6):
 class DecoderBlock:
     """One block's weights; its cache belongs to the batch that is being served."""
 
+    LAYERS = 4      # row counts whose MoE layer (buffers of its own, made for one number of rows) is kept, the last ones used
+
     def __init__(self, w: wl.Workload, heads, kv_heads, head_dim, window=0, sinks=0, seed=0, device="cuda"):
         self.w, self.heads, self.kv_heads, self.head_dim, self.window, self.sinks = w, heads, kv_heads, head_dim, window, sinks
         self.dtype = torch.bfloat16 if w.dtype == "bf16" else torch.float32
@@ -57,11 +59,17 @@ class DecoderBlock:
         else:
             o = c2r.attention_prefill(q, cache, q_start, max_new, window=self.window, sinks=self.sinks, max_kv_len=max_kv_len)
         x = x + torch.nn.functional.linear(o.view(T, H * D), self.w_o)
-        if T not in self.moe:       # (the layer's buffers are made for one number of rows)
+        return x + self._layer(T).forward(rms_norm(x))
+
+    def _layer(self, T):
+        layer = self.moe.pop(T, None)
+        if layer is None:
+            while len(self.moe) >= self.LAYERS:
+                del self.moe[next(iter(self.moe))]
             w = self.w
-            self.moe[T] = c2r.C2RLayer(T, w.d, w.E, w.K, w.F, self.dtype, self.Wg, self.bias, self.collab, *self.experts,
-                                       shared=self.shared)
-        return x + self.moe[T].forward(rms_norm(x))
+            layer = c2r.C2RLayer(T, w.d, w.E, w.K, w.F, self.dtype, self.Wg, self.bias, self.collab, *self.experts, shared=self.shared)
+        self.moe[T] = layer         # (a dict keeps its order: the last one used comes last)
+        return layer
 
 
 class Decoder:
