@@ -444,8 +444,9 @@ int c2r_distinct_devices(const int32_t *topk_idx, int64_t T, int K, int E, const
  * not stored, and no query sees them; what is cached stays as it is.  A page number outside [0, n_pages) (a page given back, say) is never
  * written and reads as page 0, which matters only if a query sees a key of it.
  * Limits (else C2R_ERR_UNSUPPORTED): head_dim 64 or 128; up to 1024 heads; batch, pages and tokens below 2^30, page_size *
- * max_pages below 2^28, batch * heads of a decoding step below 2^24.  C2R_ERR_INVALID_ARG: query heads not a multiple of kv_heads, rows or strides that are not whole 16-byte
- * pieces, strides shorter than a row.
+ * max_pages below 2^28, batch * heads of a decoding step below 2^24, T * heads + 64 * batch * kv_heads of a call for prompts below
+ * 2^29 (some larger ones pass).  C2R_ERR_INVALID_ARG: query heads not a multiple of kv_heads, rows or strides that are not whole
+ * 16-byte pieces, strides shorter than a row.
  */
 typedef struct {
     int64_t n_pages, page_size, max_pages, batch, kv_heads, head_dim, dtype, page_stride, slot_stride, head_stride;

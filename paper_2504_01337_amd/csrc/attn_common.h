@@ -201,7 +201,7 @@ struct RopeCall {
     int64_t q_bytes, k_bytes, v_bytes, q_out_bytes, k_out_bytes;
     const float *q_weight, *k_weight, *inv_freq;
     const int32_t *position, *q_start;
-    int64_t T;
+    int64_t T, first, end;  // a launch takes the tokens first .. end
     int heads, kv_heads, rot, parts;
     float eps;
     KvView kv;

@@ -85,10 +85,10 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeCall a) {
     // this lane's two 8-byte pieces of a row: bytes
     const int low = !NEIGHBOURS && turned ? c * 8 : c * 16, high = !NEIGHBOURS && turned ? a.rot * SZ / 2 + c * 8 : low + 8;
     const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t run = w / a.parts, first_token = run * TOKENS;
+    const int64_t run = w / a.parts, first_token = a.first + run * TOKENS;
     const int part = (int)(w - run * a.parts);
-    if (first_token >= a.T) return;
-    const int tokens = a.T - first_token < TOKENS ? (int)(a.T - first_token) : TOKENS;
+    if (first_token >= a.end) return;
+    const int tokens = a.end - first_token < TOKENS ? (int)(a.end - first_token) : TOKENS;
     const int total = a.heads + (CACHE ? 2 : 1) * a.kv_heads, groups = (total + HW - 1) / HW;
     u32x4 x[BATCH] = {};
     // the rows of head groups first, first + parts, ... of token t
@@ -259,15 +259,21 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeCall a) {
 }
 
 template <bool BF16, int D, bool CACHE, bool NEIGHBOURS>
-static void start(const RopeCall &a, int tokens, unsigned blocks, hipStream_t st) {
-    if (tokens == 1) qk_norm_rope_kernel<BF16, D, CACHE, NEIGHBOURS, 1><<<dim3(blocks), dim3(256), 0, st>>>(a);
-    else qk_norm_rope_kernel<BF16, D, CACHE, NEIGHBOURS, ROPE_TOKENS><<<dim3(blocks), dim3(256), 0, st>>>(a);
+static void start(RopeCall a, int tokens, hipStream_t st) {
+    // (a grid has room for so many tokens)
+    const int64_t most = (ATTN_MOST_BLOCKS - 1) * 4 / a.parts * tokens;
+    for (a.first = 0; a.first < a.T; a.first += most) {
+        a.end = a.T - a.first < most ? a.T : a.first + most;
+        const unsigned blocks = (unsigned)ceil_div(ceil_div(a.end - a.first, tokens) * a.parts, 4);
+        if (tokens == 1) qk_norm_rope_kernel<BF16, D, CACHE, NEIGHBOURS, 1><<<dim3(blocks), dim3(256), 0, st>>>(a);
+        else qk_norm_rope_kernel<BF16, D, CACHE, NEIGHBOURS, ROPE_TOKENS><<<dim3(blocks), dim3(256), 0, st>>>(a);
+    }
 }
 
 template <bool BF16, int D, bool CACHE>
-static void start(const RopeCall &a, bool neighbours, int tokens, unsigned blocks, hipStream_t st) {
-    if (neighbours) start<BF16, D, CACHE, true>(a, tokens, blocks, st);
-    else start<BF16, D, CACHE, false>(a, tokens, blocks, st);
+static void start(const RopeCall &a, bool neighbours, int tokens, hipStream_t st) {
+    if (neighbours) start<BF16, D, CACHE, true>(a, tokens, st);
+    else start<BF16, D, CACHE, false>(a, tokens, st);
 }
 
 int launch_qk_norm_rope(RopeCall a, bool bf16, int D, bool neighbours, hipStream_t st) {
@@ -279,15 +285,12 @@ int launch_qk_norm_rope(RopeCall a, bool bf16, int D, bool neighbours, hipStream
     int64_t parts = tokens > 1 ? 1 : ceil_div(8192, a.T);
     if (tokens == 1 && parts < ceil_div(groups, 4)) parts = ceil_div(groups, 4);
     a.parts = (int)(parts < groups ? parts : groups);
-    const int64_t blocks = ceil_div(ceil_div(a.T, tokens) * a.parts, 4);
-    if (blocks >= ATTN_MOST_BLOCKS) return C2R_ERR_UNSUPPORTED;
-    const unsigned n = (unsigned)blocks;
     if (bf16) {
-        if (D == 128) cache ? start<true, 128, true>(a, neighbours, tokens, n, st) : start<true, 128, false>(a, neighbours, tokens, n, st);
-        else cache ? start<true, 64, true>(a, neighbours, tokens, n, st) : start<true, 64, false>(a, neighbours, tokens, n, st);
+        if (D == 128) cache ? start<true, 128, true>(a, neighbours, tokens, st) : start<true, 128, false>(a, neighbours, tokens, st);
+        else cache ? start<true, 64, true>(a, neighbours, tokens, st) : start<true, 64, false>(a, neighbours, tokens, st);
     } else {
-        if (D == 128) cache ? start<false, 128, true>(a, neighbours, tokens, n, st) : start<false, 128, false>(a, neighbours, tokens, n, st);
-        else cache ? start<false, 64, true>(a, neighbours, tokens, n, st) : start<false, 64, false>(a, neighbours, tokens, n, st);
+        if (D == 128) cache ? start<false, 128, true>(a, neighbours, tokens, st) : start<false, 128, false>(a, neighbours, tokens, st);
+        else cache ? start<false, 64, true>(a, neighbours, tokens, st) : start<false, 64, false>(a, neighbours, tokens, st);
     }
     return launch_status();
 }

@@ -131,3 +131,21 @@ def test_lengths_past_the_cache(c2r, dtype, most, window, sinks):
     kk, vv = k[last].contiguous(), v[last].contiguous()
     c2r.qk_norm_rope_append(one, kk, vv, bt.cache, f, None, None, w, w)
     assert torch.equal(bt.cache.k, before_k) and torch.equal(bt.cache.v, before_v)       # they were there, or have no place
+
+
+# ---- sizes past a grid ----
+
+def test_norm_rope_of_more_tokens_than_a_grid_takes(c2r):
+    """2^27 + 5 tokens, in place: rows everywhere have the bits that a short call gives them, so each was turned once."""
+    T, D = (1 << 27) + 5, 64
+    q, k = (torch.empty((T, 1, D), dtype=torch.bfloat16, device="cuda").normal_() for _ in "qk")
+    pos = torch.arange(T, dtype=torch.int32, device="cuda") % 100003
+    from test_gpu_attention import _freq
+    f, w = _freq(D), _randn(np.random.default_rng(55), D)
+    at = torch.cat([torch.arange(c - 9, c + 9) for c in (9, 1 << 24, (1 << 25) - 4, 1 << 25, 3 << 24, (1 << 26) - 8, (1 << 26) - 4, 1 << 26, T - 9)]
+                   + [torch.randint(0, T, (4000,), generator=torch.Generator().manual_seed(1))]).cuda()
+    want = c2r.qk_norm_rope(q[at], k[at], f, pos[at], w, w)
+    c2r.qk_norm_rope(q, k, f, pos, w, w, out=(q, k))
+    assert torch.equal(q[at], want[0]) and torch.equal(k[at], want[1])
+    del q, k
+    torch.cuda.empty_cache()
