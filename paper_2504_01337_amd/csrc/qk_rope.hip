@@ -3,25 +3,26 @@
 //     y = x * rsqrt(mean(x^2) + eps) * w          (no norm without weights)
 //     the first R elements in pairs (i, j): y_i cos - y_j sin, y_j cos + y_i sin at the angle position * inv_freq[i]
 //
-// A lane holds 16 bytes of a head's row, D * size / 16 lanes a head; a wave takes the heads of ONE token in turn, four groups of
-// them in flight, so the angles of its elements are worked out once a token.  The angle is a product in 64 bits, in turns, less
-// its whole turns: at position 100000 a 32-bit product would be off by 4e-3 radians, more than bf16 resolves.  v_sin_f32 and
-// v_cos_f32 take turns and are within 1.3e-7 of sin and cos over one turn (2^20 arguments tried).  Everything is 32 bits wide up
-// to the one rounding.
+// A lane holds 16 bytes of a head's row, a whole pair or several, D * size / 16 lanes a head; a wave takes head groups of one token in
+// turn, four of them in flight, so the angles of its elements are worked out once.  The angle is a product in 64 bits, in turns,
+// less its whole turns: at position 100000 a 32-bit product would be off by 4e-3 radians, more than bf16 resolves.  Everything else is
+// 32 bits wide up to the one rounding.
 // Memory bound for many tokens: every row is read and written once.  8192 tokens, 16 query and 16 key heads of 128, bf16, 201 MB
-// with the appended values: 43 us, 4.7 TB/s (a large copy runs at 4.9); without a cache, 134 MB, 26.7 us, 5.0 TB/s.  Few tokens: a
-// chain of loads (sequence, length, page) behind a launch, 4.5 us for 1 to 64 tokens.
+// with the appended values: 42 us, 4.8 TB/s (a large copy runs at 4.9); without a cache, 134 MB, 26.5 us, 5.1 TB/s.  Few tokens: a
+// chain of loads (sequence, length, page) behind a launch, 3.7 us for 1 token, 4.1 for 64 (in a graph).
 #include <type_traits>
 
 #include "attn_common.h"
 
 namespace c2r {
 
-// Waves of one token and of ROPE_TOKENS tokens: a launch that would have ROPE_MANY waves or more at a token each, all heads of
-// the token in one wave (four groups of heads), takes the second.  us with one, two and four tokens a wave (bf16, D 128): 8192
-// tokens of 16/16 heads 49.2, 43.0, 44.2, without a cache 30.6, 26.7, 28.2; 16000 of 32/4 heads 80.6, 69.2, 67.5; 4096 of 32/32
-// 37.8, 40.1, 56.5; pairs of neighbours 31.0, 29.5, 36.6.  Below: 2000 tokens of 16/16 19.0 and 19.8, 1301 of 32/8, half of a head turned, 14.1 and 18.1.
-constexpr int ROPE_TOKENS = 2, ROPE_MANY = 8192;
+// Waves of a token: enough that the call has ROPE_WAVES of them, and one for every ROPE_GROUPS head groups.  us, 1, 2, 3, 4, 6, 12
+// waves a token (bf16, heads of 128, in a stream of calls, its host time of 10.5 in the smallest): 1000 tokens of 16/16 heads (12 groups)
+// 11.4, 10.5, 10.5, 10.5, 10.7, 13.3; 2731 16.4, 17.0, 18.1, 19.7, 21.0, 27.3; 8192 43.1, 44.8, 49.1, 52.7, 58.4, 85.7; 1400 of 64/32 (32
+// groups) 24.4, 19.9, 19.8, 19.1, 21.9, 25.2; 8192 110, 107, 104, 104, 110, 129.  In a graph, 300 of 16/16 9.6, 6.9, 5.8, 5.9, 5.3, 5.9.
+// (Two tokens in a row to a wave, whose places are looked up side by side: 8192 of 16/16 42.1, but 2731 20.9, 12000 60.4 where one token
+// takes 55.4.)
+constexpr int ROPE_WAVES = 2600, ROPE_GROUPS = 12;
 
 // The sequence that row t belongs to, or -1 past the last one: how many of q_start[0 .. batch] are at most t.
 __device__ __forceinline__ int sequence_of(const int32_t *q_start, int batch, int64_t t) {
@@ -72,12 +73,10 @@ __device__ __forceinline__ void direction(double r, float &c, float &s) {
     }
 }
 
-// TOKENS: tokens in a row that a wave takes.  Their places are looked up side by side, a lane each: the chain of loads behind a
-// place (sequence, length, page) is what a wave that is only just long enough for one token spends its life on.
 // Both elements of a pair are in one lane: neighbours stand in its 16 bytes; of halves, a lane of the turned part takes 8 bytes
 // of each.  (16 bytes in a row of either and the partners' by an exchange, normed and turned twice: 52.3 us for the 8192 tokens with
-// their append, where this takes 43.0; 1301 tokens, half of a head turned 18.6, 14.1.)
-template <bool BF16, int D, bool CACHE, bool NEIGHBOURS, int TOKENS>
+// their append, where this took 43.0; 1301 tokens, half of a head turned 18.6, 14.1.)
+template <bool BF16, int D, bool CACHE, bool NEIGHBOURS>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeCall a) {
     constexpr int SZ = BF16 ? 2 : 4, EPL = 16 / SZ, LH = D / EPL, HW = 64 / LH, BATCH = 4;
     const int lane = lane_id(), sub = lane / LH, c = lane % LH;
@@ -85,14 +84,13 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeCall a) {
     // this lane's two 8-byte pieces of a row: bytes
     const int low = !NEIGHBOURS && turned ? c * 8 : c * 16, high = !NEIGHBOURS && turned ? a.rot * SZ / 2 + c * 8 : low + 8;
     const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t run = w / a.parts, first_token = a.first + run * TOKENS;
+    const int64_t run = w / a.parts, t = a.first + run;
     const int part = (int)(w - run * a.parts);
-    if (first_token >= a.end) return;
-    const int tokens = a.end - first_token < TOKENS ? (int)(a.end - first_token) : TOKENS;
+    if (t >= a.end) return;
     const int total = a.heads + (CACHE ? 2 : 1) * a.kv_heads, groups = (total + HW - 1) / HW;
     u32x4 x[BATCH] = {};
-    // the rows of head groups first, first + parts, ... of token t
-    auto fetch = [&](int64_t t, int first) {
+    // the rows of head groups first, first + parts, ...
+    auto fetch = [&](int first) {
 #pragma unroll
         for (int u = 0; u < BATCH; ++u) {
             const int h = (first + u * a.parts) * HW + sub;
@@ -116,54 +114,23 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeCall a) {
             *reinterpret_cast<u32x4 *>(row + low) = v;
         }
     };
-    fetch(first_token, part);  // on its way while the places are looked up
+    fetch(part);  // on its way while the token's place is looked up
 
-    // ---- lane i: token i's position, and its row's bytes from the cache's start (-1: no such place; -2: of no sequence) ----
+    // ---- the token's position, and its row's bytes from the cache's start (-1: no such place) ----
     int pos = 0;
     int64_t place = -1;
-    const int64_t mine = first_token + (lane < tokens ? lane : tokens - 1);
     if constexpr (CACHE) {
-        int b = (int)mine;
-        if (a.q_start) {
-            // the first token's sequence, and how many of the next 64 begin by each of the others
-            const int b0 = sequence_of(a.q_start, a.kv.batch, first_token);
-            b = b0;
-            if constexpr (TOKENS > 1) {
-                // (rows before the first sequence and past the last one are of none: b0 = -1 either way)
-                const bool before = first_token < a.q_start[0];
-                const int from = b0 < 0 ? (before ? 0 : a.kv.batch + 1) : b0 + 1, at = from + lane;
-                const int64_t begins = at <= a.kv.batch ? a.q_start[at] : INT64_MAX;
-#pragma unroll
-                for (int i = 1; i < TOKENS; ++i) {
-                    const int n = __popcll(__ballot(begins <= first_token + i));
-                    if (lane != i || i >= tokens) continue;
-                    // 64 empty sequences in a row: look again from the start
-                    b = n == 64 ? -3 : n == 0 ? b0 : from + n - 1;
-                    if (b == a.kv.batch) b = -1;
-                }
-                uint64_t again = __ballot(b == -3);
-                while (again) {
-                    const int i = __ffsll((unsigned long long)again) - 1;
-                    again &= again - 1;
-                    const int found = sequence_of(a.q_start, a.kv.batch, first_token + i);
-                    if (lane == i) b = found;
-                }
-            }
-        }
-        if (b < 0) {
-            place = -2;
-        } else if (lane < tokens) {
-            const int len = max(a.kv.kv_len[b], 0);
-            int64_t end = mine + 1;
-            if (a.q_start) end = a.q_start[b + 1] < a.T ? a.q_start[b + 1] : a.T;
-            pos = len - (int)(end - mine);
-            if (pos >= 0 && pos < a.kv.capacity) {  // (past the end there is no place, and the tokens before it stay)
-                const int page = a.kv.table[(int64_t)b * a.kv.max_pages + a.kv.page_of(pos)];
-                if ((uint32_t)page < (uint32_t)a.kv.n_pages) place = a.kv.offset(page, pos);
-            }
+        const int b = a.q_start ? sequence_of(a.q_start, a.kv.batch, t) : (int)t;
+        if (b < 0) return;  // a row of no sequence
+        int64_t end = t + 1;
+        if (a.q_start) end = a.q_start[b + 1] < a.T ? a.q_start[b + 1] : a.T;
+        pos = max(a.kv.kv_len[b], 0) - (int)(end - t);
+        if (pos >= 0 && pos < a.kv.capacity) {  // (past the end there is no place, and the tokens before it stay)
+            const int page = a.kv.page(b, pos);
+            if ((uint32_t)page < (uint32_t)a.kv.n_pages) place = a.kv.offset(page, pos);
         }
     }
-    if (a.position) pos = a.position[mine];
+    if (a.position) pos = a.position[t];
 
     // weights of this lane's elements
     float wq[EPL], wk[EPL];
@@ -195,103 +162,84 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeCall a) {
         }
     };
 
-    for (int i = 0; i < tokens; ++i) {
-        const int64_t t = first_token + i;
-        const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)place, i), hi = __builtin_amdgcn_readlane((uint32_t)(place >> 32), i);
-        const int64_t cache_off = (int64_t)((uint64_t)hi << 32 | lo);
-        const int p = __builtin_amdgcn_readlane(pos, i);
-        // the angles of this lane's elements at this token
-        float cs[NA], sn[NA];
+    // the angles of this lane's elements
+    float cs[NA], sn[NA];
 #pragma unroll
-        for (int k = 0; k < NA; ++k) {
-            const double turns = (double)p * ((double)freq[k] * 0.15915494309189533577);
-            direction<BF16>(turns - __builtin_rint(turns), cs[k], sn[k]);
-        }
-        for (int first = part; first < groups; first += BATCH * a.parts) {
-            u32x4 now[BATCH];
+    for (int k = 0; k < NA; ++k) {
+        const double turns = (double)pos * ((double)freq[k] * 0.15915494309189533577);
+        direction<BF16>(turns - __builtin_rint(turns), cs[k], sn[k]);
+    }
+    for (int first = part; first < groups; first += BATCH * a.parts) {
+        u32x4 now[BATCH];
 #pragma unroll
-            for (int u = 0; u < BATCH; ++u) now[u] = x[u];
-            // the next rows, of this token or the next one
-            if (first + BATCH * a.parts < groups) fetch(t, first + BATCH * a.parts);
-            else if (i + 1 < tokens) fetch(t + 1, part);
-            if (cache_off == -2) continue;  // rows of no sequence
+        for (int u = 0; u < BATCH; ++u) now[u] = x[u];
+        if (first + BATCH * a.parts < groups) fetch(first + BATCH * a.parts);
 #pragma unroll
-            for (int u = 0; u < BATCH; ++u) {
-                const int hg = first + u * a.parts;
-                if (hg >= groups) break;
-                const int h = hg * HW + sub;
-                const bool is_q = h < a.heads, is_v = h >= a.heads + a.kv_heads, real = h < total;
-                float y[EPL];
-                unpack(now[u], y);
-                float sq = 0.0f;
+        for (int u = 0; u < BATCH; ++u) {
+            const int hg = first + u * a.parts;
+            if (hg >= groups) break;
+            const int h = hg * HW + sub;
+            const bool is_q = h < a.heads, is_v = h >= a.heads + a.kv_heads, real = h < total;
+            float y[EPL];
+            unpack(now[u], y);
+            float sq = 0.0f;
 #pragma unroll
-                for (int k = 0; k < EPL; ++k) sq = __builtin_fmaf(y[k], y[k], sq);
-                sq = head_sum<LH>(sq);
-                float rs = 1.0f;
+            for (int k = 0; k < EPL; ++k) sq = __builtin_fmaf(y[k], y[k], sq);
+            sq = head_sum<LH>(sq);
+            float rs = 1.0f;
 #if defined(__HIP_DEVICE_COMPILE__)
-                if (is_q ? a.q_weight != nullptr : a.k_weight != nullptr) rs = __builtin_amdgcn_rsqf(__builtin_fmaf(sq, 1.0f / D, a.eps));
+            if (is_q ? a.q_weight != nullptr : a.k_weight != nullptr) rs = __builtin_amdgcn_rsqf(__builtin_fmaf(sq, 1.0f / D, a.eps));
 #endif
 #pragma unroll
-                for (int k = 0; k < EPL; ++k) y[k] = y[k] * rs * (is_q ? wq[k] : wk[k]);
-                float out[EPL];
+            for (int k = 0; k < EPL; ++k) y[k] = y[k] * rs * (is_q ? wq[k] : wk[k]);
+            float out[EPL];
 #pragma unroll
-                for (int k = 0; k < NA; ++k) {
-                    const int i = NEIGHBOURS ? 2 * k : k, j = NEIGHBOURS ? 2 * k + 1 : k + NA;
-                    out[i] = turned ? y[i] * cs[k] - y[j] * sn[k] : y[i];
-                    out[j] = turned ? y[j] * cs[k] + y[i] * sn[k] : y[j];
-                }
-                u32x4 r;
+            for (int k = 0; k < NA; ++k) {
+                const int i = NEIGHBOURS ? 2 * k : k, j = NEIGHBOURS ? 2 * k + 1 : k + NA;
+                out[i] = turned ? y[i] * cs[k] - y[j] * sn[k] : y[i];
+                out[j] = turned ? y[j] * cs[k] + y[i] * sn[k] : y[j];
+            }
+            u32x4 r;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) r[k] = BF16 ? pack_bf16x2(out[(2 * k) % EPL], out[(2 * k + 1) % EPL]) : __float_as_uint(out[k]);
-                if (!real) continue;
-                if (is_q) {
-                    store(a.q_out + t * a.q_out_bytes + (int64_t)h * (D * SZ), r);
-                } else if constexpr (!CACHE) {
-                    store(a.k_out + t * a.k_out_bytes + (int64_t)(h - a.heads) * (D * SZ), r);
-                } else if (cache_off >= 0) {
-                    const int kh = h - a.heads - (is_v ? a.kv_heads : 0);
-                    unsigned char *base = const_cast<unsigned char *>(is_v ? a.kv.v : a.kv.k);
-                    store(base + cache_off + kh * a.kv.head_bytes, is_v ? now[u] : r);
-                }
+            for (int k = 0; k < 4; ++k) r[k] = BF16 ? pack_bf16x2(out[(2 * k) % EPL], out[(2 * k + 1) % EPL]) : __float_as_uint(out[k]);
+            if (!real) continue;
+            if (is_q) {
+                store(a.q_out + t * a.q_out_bytes + (int64_t)h * (D * SZ), r);
+            } else if constexpr (!CACHE) {
+                store(a.k_out + t * a.k_out_bytes + (int64_t)(h - a.heads) * (D * SZ), r);
+            } else if (place >= 0) {
+                const int kh = h - a.heads - (is_v ? a.kv_heads : 0);
+                unsigned char *base = const_cast<unsigned char *>(is_v ? a.kv.v : a.kv.k);
+                store(base + place + kh * a.kv.head_bytes, is_v ? now[u] : r);
             }
         }
     }
 }
 
 template <bool BF16, int D, bool CACHE, bool NEIGHBOURS>
-static void start(RopeCall a, int tokens, hipStream_t st) {
+static void start(RopeCall a, hipStream_t st) {
     // (a grid has room for so many tokens)
-    const int64_t most = (ATTN_MOST_BLOCKS - 1) * 4 / a.parts * tokens;
+    const int64_t most = (ATTN_MOST_BLOCKS - 1) * 4 / a.parts;
     for (a.first = 0; a.first < a.T; a.first += most) {
         a.end = a.T - a.first < most ? a.T : a.first + most;
-        const unsigned blocks = (unsigned)ceil_div(ceil_div(a.end - a.first, tokens) * a.parts, 4);
-        if (tokens == 1) qk_norm_rope_kernel<BF16, D, CACHE, NEIGHBOURS, 1><<<dim3(blocks), dim3(256), 0, st>>>(a);
-        else qk_norm_rope_kernel<BF16, D, CACHE, NEIGHBOURS, ROPE_TOKENS><<<dim3(blocks), dim3(256), 0, st>>>(a);
+        qk_norm_rope_kernel<BF16, D, CACHE, NEIGHBOURS><<<dim3((unsigned)ceil_div((a.end - a.first) * a.parts, 4)), dim3(256), 0, st>>>(a);
     }
 }
 
-template <bool BF16, int D, bool CACHE>
-static void start(const RopeCall &a, bool neighbours, int tokens, hipStream_t st) {
-    if (neighbours) start<BF16, D, CACHE, true>(a, tokens, st);
-    else start<BF16, D, CACHE, false>(a, tokens, st);
+template <bool BF16, int D>
+static void start(const RopeCall &a, bool cache, bool neighbours, hipStream_t st) {
+    if (cache) neighbours ? start<BF16, D, true, true>(a, st) : start<BF16, D, true, false>(a, st);
+    else neighbours ? start<BF16, D, false, true>(a, st) : start<BF16, D, false, false>(a, st);
 }
 
 int launch_qk_norm_rope(RopeCall a, bool bf16, int D, bool neighbours, hipStream_t st) {
     const bool cache = a.k_out == nullptr;
-    const int lanes = D * (bf16 ? 2 : 4) / 16, groups = (int)ceil_div(a.heads + (cache ? 2 : 1) * a.kv_heads, 64 / lanes);
-    // Few tokens: waves for every four head groups, down to one, while the chip has room.  Many: a wave takes all head groups of
-    // ROPE_TOKENS tokens.
-    const int tokens = a.T * ceil_div(groups, 4) >= ROPE_MANY ? ROPE_TOKENS : 1;
-    int64_t parts = tokens > 1 ? 1 : ceil_div(8192, a.T);
-    if (tokens == 1 && parts < ceil_div(groups, 4)) parts = ceil_div(groups, 4);
+    const int lanes = D * (bf16 ? 2 : 4) / 16;
+    const int64_t groups = ceil_div(a.heads + (cache ? 2 : 1) * a.kv_heads, 64 / lanes);
+    const int64_t fill = ceil_div(ROPE_WAVES, a.T), share = ceil_div(groups, ROPE_GROUPS), parts = fill > share ? fill : share;
     a.parts = (int)(parts < groups ? parts : groups);
-    if (bf16) {
-        if (D == 128) cache ? start<true, 128, true>(a, neighbours, tokens, st) : start<true, 128, false>(a, neighbours, tokens, st);
-        else cache ? start<true, 64, true>(a, neighbours, tokens, st) : start<true, 64, false>(a, neighbours, tokens, st);
-    } else {
-        if (D == 128) cache ? start<false, 128, true>(a, neighbours, tokens, st) : start<false, 128, false>(a, neighbours, tokens, st);
-        else cache ? start<false, 64, true>(a, neighbours, tokens, st) : start<false, 64, false>(a, neighbours, tokens, st);
-    }
+    if (bf16) D == 128 ? start<true, 128>(a, cache, neighbours, st) : start<true, 64>(a, cache, neighbours, st);
+    else D == 128 ? start<false, 128>(a, cache, neighbours, st) : start<false, 64>(a, cache, neighbours, st);
     return launch_status();
 }
 

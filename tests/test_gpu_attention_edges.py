@@ -149,3 +149,48 @@ def test_norm_rope_of_more_tokens_than_a_grid_takes(c2r):
     assert torch.equal(q[at], want[0]) and torch.equal(k[at], want[1])
     del q, k
     torch.cuda.empty_cache()
+
+
+# ---- norms and rotation: every form over few and many tokens ----
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,R", [(64, 64), (64, 16), (128, 128), (128, 64)])
+@pytest.mark.parametrize("nb", [False, True])
+@pytest.mark.parametrize("H,Hkv,T", [(5, 1, 2599), (30, 15, 2601), (16, 8, 8197), (1, 1, 1301)])
+def test_norm_rope_forms(c2r, dtype, D, R, nb, H, Hkv, T):
+    """Dense, in place and into a cache with positions of their own: the same bits.  Sizes on both sides of where a token's heads are
+    spread over waves, head groups that are not full, an odd number of tokens; a few rows against 64 bits."""
+    from test_gpu_attention import _check_rope, _freq
+    rng = np.random.default_rng(56 + D + R + H)
+    qkv = torch.randn((T, H + 2 * Hkv, D), generator=torch.Generator(device="cuda").manual_seed(H), device="cuda").to(
+        torch.bfloat16 if dtype == "bf16" else torch.float32)
+    q, k, v = qkv[:, :H], qkv[:, H:H + Hkv], qkv[:, H + Hkv:]
+    wq, wk, f = _randn(rng, D), _randn(rng, D), _freq(R)
+    pos = rng.integers(0, 1 << 17, T).astype(np.int32)
+    p = torch.from_numpy(pos).cuda()
+    qo, ko = c2r.qk_norm_rope(q, k, f, p, wq, wk, 1e-5, nb)
+    some = np.unique(np.concatenate([[0, 1, T - 2, T - 1], rng.integers(0, T, 60)]))
+    at = torch.from_numpy(some).cuda()
+    _check_rope(qo[at], q[at], wq, 1e-5, f, pos[some], nb, dtype)
+    _check_rope(ko[at], k[at], wk, 1e-5, f, pos[some], nb, dtype)
+    # sequences of one, of none, of odd lengths; one row before the first and two behind the last
+    cuts = np.sort(np.concatenate([[1, 1, T - 2, T - 2], rng.integers(1, T - 1, 7)])).astype(np.int32)
+    B, page = len(cuts) - 1, 48
+    lens = np.diff(cuts)
+    need = -(-lens // page)
+    table = np.full((B, int(need.max())), -1, dtype=np.int32)
+    table[np.arange(table.shape[1])[None] < need[:, None]] = rng.permutation(int(need.sum())).astype(np.int32)
+    kk, vv = (torch.full((int(need.sum()), Hkv, page, D), 3.0, dtype=qkv.dtype, device="cuda") for _ in "kv")
+    cache = c2r.PagedKVCache(kk, vv, torch.from_numpy(table).cuda(), torch.from_numpy(lens.astype(np.int32)).cuda())
+    out = torch.full((T, H, D), 9.0, dtype=qkv.dtype, device="cuda")
+    c2r.qk_norm_rope_append(q, k, v, cache, f, torch.from_numpy(cuts).cuda(), p, wq, wk, 1e-5, nb, out=out)
+    assert (out[:1] == 9).all() and (out[T - 2:] == 9).all() and torch.equal(out[1:T - 2], qo[1:T - 2])
+    seq = np.repeat(np.arange(B), lens)
+    place = np.concatenate([np.arange(n) for n in lens])
+    pages, slots = torch.from_numpy(table[seq, place // page].astype(np.int64)).cuda(), torch.from_numpy(place % page).cuda()
+    assert torch.equal(kk[pages, :, slots], ko[1:T - 2]) and torch.equal(vv[pages, :, slots], v[1:T - 2])
+    kk[pages, :, slots], vv[pages, :, slots] = 3.0, 3.0
+    assert (kk == 3).all() and (vv == 3).all()
+    rest = v.clone()
+    c2r.qk_norm_rope(q, k, f, p, wq, wk, 1e-5, nb, out=(q, k))
+    assert torch.equal(q, qo) and torch.equal(k, ko) and torch.equal(v, rest)
