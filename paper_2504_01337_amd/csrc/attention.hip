@@ -167,6 +167,7 @@ static int attention_call(const void *q, int64_t q_stride, int64_t T, int heads,
     a.window = window >= ATTN_MOST ? 0 : (int)window;
     a.sinks = a.window == 0 ? 0 : sinks > capacity ? (int)capacity : (int)sinks;
     a.scale_log2 = scale * 1.4426950408889634f;
+    a.scale_size = a.scale_log2 == 0.0f ? 1.0f : fabsf(a.scale_log2);
     a.splits = 1;
     return C2R_OK;
 }

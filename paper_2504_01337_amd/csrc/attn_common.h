@@ -67,6 +67,7 @@ struct AttnCall {
     int heads, group;         // query heads, and of them per key head
     int window, sinks;        // window 0: none
     float scale_log2;         // scale * log2(e): the softmax is taken in powers of two
+    float scale_size;         // its absolute value, or 1 where it is 0
     int splits, split_tiles;  // the key tiles of one row of blocks, cut after every split_tiles; 1: no partial results
     // Prompts: blocks of rows for every key head and part.  by_rows: counted through all sequences, T * group / BM + batch of them;
     // else as many for each sequence as max_q needs.

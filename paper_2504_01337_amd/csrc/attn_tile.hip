@@ -90,7 +90,10 @@ __device__ __forceinline__ float add_pair(float v, uint32_t pair) {
 // ALIGNED: pages of whole groups of 16 keys, and of less than 4 GB, so that the 16 rows which a wave copies of a tile lie in
 // one page: one look-up and one scalar address.  Working out every lane's page takes as many vector instructions per tile as
 // the softmax.
-template <int D, bool ALIGNED>
+// ANY_SCALE: the loop takes maxima of scores before their scale and hides keys by scores of -infinity, so the scale there is positive.
+// A negative one becomes the queries' sign, and with 0 the queries are 0 (or NaN, where the definition gives one).  A form of its own,
+// as this costs every block some 0.2 us: 32 prompts of 300 43.4 us for 42.7.
+template <int D, bool ALIGNED, bool ANY_SCALE>
 __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void attn_tile_kernel(AttnCall a) {
     using T = TileShape<D>;
     constexpr int KT = T::KT, KSTEPS = D / 16, DT = D / 32, VALU = 0x2, MFMA = 0x8, DS_READ = 0x100;
@@ -120,6 +123,17 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void attn_tile_kernel(AttnCa
     bf16x8 q[KSTEPS];
 #pragma unroll
     for (int s = 0; s < KSTEPS; ++s) q[s] = *reinterpret_cast<const bf16x8 *>(q_row + s * 32 + h * 16);
+    if constexpr (ANY_SCALE) {
+        const float sign = a.scale_log2 < 0.0f ? -1.0f : a.scale_log2 > 0.0f ? 1.0f : 0.0f;
+#pragma unroll
+        for (int s = 0; s < KSTEPS; ++s) {
+            u32x4 w = __builtin_bit_cast(u32x4, q[s]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) w[c] = pack_bf16x2(__uint_as_float(w[c] << 16) * sign, __uint_as_float(w[c] & 0xffff0000u) * sign);
+            q[s] = __builtin_bit_cast(bf16x8, w);
+        }
+    }
+    const float scale = ANY_SCALE ? a.scale_size : a.scale_log2;
 
     const KeyTiles<KT> tiles(a, bp_min, bp_max);
     int x0, x1;
@@ -272,8 +286,8 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void attn_tile_kernel(AttnCa
         auto weigh = [&](int u) {
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
-                const float lo = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], a.scale_log2, -m));
-                const float hi = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e + 1], a.scale_log2, -m));
+                const float lo = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], scale, -m));
+                const float hi = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e + 1], scale, -m));
                 const uint32_t pair = pack_bf16x2(lo, hi);
                 w[u][e >> 3][(e >> 1) & 3] = pair;
                 l = add_pair(l, pair);
@@ -314,7 +328,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void attn_tile_kernel(AttnCa
                 if (!whole) mask(u);
                 here = fmaxf(here, largest(u));
             }
-            top = fmaxf(top, max_halves(here) * a.scale_log2);
+            top = fmaxf(top, max_halves(here) * scale);
             if (bare && top != -__builtin_inff()) m = __builtin_ceilf(top), bare = false;
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -375,7 +389,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void attn_tile_kernel(AttnCa
             add(1, d / DT, d % DT);
             if (d < DT) read_values(1, 1, d);
         }
-        top = max_halves(fmaxf(part, largest(1))) * a.scale_log2;
+        top = max_halves(fmaxf(part, largest(1))) * scale;
         STRETCH(DT, 2, 2)
         STRETCH(DT, 0, 2)
         asm volatile("" : "+v"(top));
@@ -451,8 +465,9 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void attn_tile_kernel(AttnCa
 int launch_attn_tile(const AttnCall &a, int D, hipStream_t st) {
     const dim3 grid((unsigned)((int64_t)a.splits * a.kv.kv_heads * a.row_blocks * (a.by_rows ? 1 : a.kv.batch))), block(256);
     const bool aligned = a.kv.page_size % 16 == 0 && a.kv.page_bytes < (1ll << 32) && a.kv.page_size * a.kv.slot_bytes < (1ll << 32);
-    if (D == 128) aligned ? attn_tile_kernel<128, true><<<grid, block, 0, st>>>(a) : attn_tile_kernel<128, false><<<grid, block, 0, st>>>(a);
-    else aligned ? attn_tile_kernel<64, true><<<grid, block, 0, st>>>(a) : attn_tile_kernel<64, false><<<grid, block, 0, st>>>(a);
+    if (!(a.scale_log2 > 0.0f)) D == 128 ? attn_tile_kernel<128, false, true><<<grid, block, 0, st>>>(a) : attn_tile_kernel<64, false, true><<<grid, block, 0, st>>>(a);
+    else if (D == 128) aligned ? attn_tile_kernel<128, true, false><<<grid, block, 0, st>>>(a) : attn_tile_kernel<128, false, false><<<grid, block, 0, st>>>(a);
+    else aligned ? attn_tile_kernel<64, true, false><<<grid, block, 0, st>>>(a) : attn_tile_kernel<64, false, false><<<grid, block, 0, st>>>(a);
     const int rc = launch_status();
     return rc == C2R_OK && a.splits > 1 ? launch_attn_join(a, true, D, st) : rc;
 }

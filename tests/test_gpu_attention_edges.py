@@ -194,3 +194,55 @@ def test_norm_rope_forms(c2r, dtype, D, R, nb, H, Hkv, T):
     rest = v.clone()
     c2r.qk_norm_rope(q, k, f, p, wq, wk, 1e-5, nb, out=(q, k))
     assert torch.equal(q, qo) and torch.equal(k, ko) and torch.equal(v, rest)
+
+
+# ---- scales of either sign ----
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_across_parts_for_either_sign(c2r, dtype, D, sign):
+    """Scores (powers of two) of 126.5 in the first tile of keys, 0 behind it but for one of 127.5 half way: the last one counts for 2 of
+    66 parts, in whichever part of the keys it comes."""
+    rng = np.random.default_rng(57 + D)
+    new, n, scale = 8, 3000, sign * float(np.log(2.0)) / 2
+    bt = Batch(c2r, rng, dtype, D, 1, 16, [n], [new])
+    k, v = bt.rows[0]
+    k.zero_(), v.zero_()
+    k[:64, 0, 0], k[1500, 0, 0] = 253.0 * sign, 255.0 * sign
+    v[1500] = 1.0
+    bt.write(0, k, v)
+    q = _randn(rng, new, 2, D, dtype=dtype)
+    q[..., 0] = 1.0
+    got = _np(c2r.attention_prefill(q, bt.cache, bt.q_start, new, scale))
+    got1 = _np(c2r.attention_decode(q[-1:], bt.cache, scale))
+    for g, first in ((got, n - new), (got1, n - 1)):
+        ref, size, spread = oa.attention(_np(q[len(q) - len(g):]), _np(k), _np(v), first, scale)
+        assert np.abs(ref - 2 / 66).max() < 1e-6
+        # (a score has one term that is not zero: no sum of D roundings)
+        assert (np.abs(g - ref) <= 8 * U * spread * size + (2 * n + 16) * U * size + (2 * B8 * size if dtype == "bf16" else 0)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [-1.0, 0.0])
+def test_scales_that_are_not_positive_of_long_prompts(c2r, dtype, scale):
+    """Prompts whose keys are split, with NaN in a query, in a hidden and in a visible place."""
+    rng = np.random.default_rng(58)
+    D, new, lens = 64, [130, 70], [1200, 70]
+    bt = Batch(c2r, rng, dtype, D, 1, 16, lens, new)
+    q = _randn(rng, 200, 2, D, dtype=dtype)
+    q[7, 1, 5] = float("nan")
+    for b, j in ((0, 1150), (1, 40)):
+        bt.rows[b][0][j, 0, 3] = float("nan")
+        bt.write(b, *bt.rows[b])
+    got = c2r.attention_prefill(q, bt.cache, bt.q_start, 130, scale)
+    nan = torch.zeros((200, 2), dtype=torch.bool, device="cuda")
+    nan[80:130], nan[130 + 40:], nan[7, 1] = True, True, True
+    assert torch.isnan(got[nan]).all() and torch.isfinite(got[~nan]).all()
+    qn, clean = _np(q), ~nan.cpu().numpy()
+    for b, (t, m) in enumerate(((0, 130), (130, 70))):
+        k, v = (_np(x) for x in bt.rows[b])
+        ref, size, spread = oa.attention(qn[t:t + m], k, v, lens[b] - m, scale)
+        tol = _sums(D, lens[b], size, spread) + (B8 * (size + np.abs(ref)) if dtype == "bf16" else 0.0)
+        ok = clean[t:t + m]
+        assert (np.abs(_np(got[t:t + m]) - ref) <= tol)[ok].all()
