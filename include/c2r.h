@@ -493,7 +493,7 @@ int c2r_qk_norm_rope_append(const void *q, int64_t q_stride, const void *k, int6
  * beside a window.  A sequence without a visible key (kv_len 0, say) gets zeros.  What is hidden has no part in the result, an
  * infinity or a NaN there included.  Scores, softmax and sums in 32 bits (bf16: the products' weights keep 16 of them), rounded
  * once.  Long caches are split over the GPU and joined, with the same bits on every run.
- * q, out     : [batch, heads, head_dim] of the cache's dtype, strides as in c2r_qk_norm_rope
+ * q, out     : [batch, heads, head_dim] of the cache's dtype, strides as in c2r_qk_norm_rope; out may be q (same stride)
  * max_kv_len : host; the longest kv_len of the batch (0: not known).  It only steers the split: results hold for any value.
  * ws         : c2r_workspace_bytes(C2R_STAGE_ATTENTION, batch, head_dim, heads, kv_heads, 0, dtype) bytes, 256-aligned
  */

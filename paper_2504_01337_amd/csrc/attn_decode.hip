@@ -39,7 +39,7 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void attn_decode_kernel(Attn
     S::template run<4>(a, q, st, tiles, x0 + wave, x1, b, kv_head * a.kv.head_bytes, p, p, p);
     uint32_t redo = S::finish(st, left);
     float *mine = join_o + wave * 16 * D;
-    if (n < left) {
+    if (n < left && !(redo >> n & 1)) {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll

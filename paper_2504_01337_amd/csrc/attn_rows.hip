@@ -61,7 +61,7 @@ __global__ __launch_bounds__(256, 3) void attn_rows_kernel(AttnCall a) {
             if (ml) a.part_ml[pr * 2] = m, a.part_ml[pr * 2 + 1] = a.blind(pos) || x0 == x1 ? PART_EMPTY : l;
         }
     };
-    if (n < left) {
+    if (n < left && !(redo >> n & 1)) {  // (a row is written once: `out` may be q, which the exact row reads)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             float v[S::VEL];

@@ -411,7 +411,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void attn_tile_kernel(AttnCa
     redo = (redo | redo >> 32) & 0xffffffffu;
 
     // ---- results: lane (h, n), word e of o[d]: element 32 d + 8 (e / 4) + 4 h + e % 4 of row n ----
-    if (n < left) {
+    if (n < left && !(redo >> n & 1)) {  // (a row is written once: `out` may be q, which the exact row reads)
         if (uncut) {
             const float inv = a.blind(p) ? 0.0f : 1.0f / l;
             unsigned char *out = a.out + token * a.out_bytes + (int64_t)head * (D * 2);

@@ -246,3 +246,27 @@ def test_scales_that_are_not_positive_of_long_prompts(c2r, dtype, scale):
         tol = _sums(D, lens[b], size, spread) + (B8 * (size + np.abs(ref)) if dtype == "bf16" else 0.0)
         ok = clean[t:t + m]
         assert (np.abs(_np(got[t:t + m]) - ref) <= tol)[ok].all()
+
+
+# ---- results in the place of the queries ----
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,context,window", [(64, 0, 30), (128, 0, 30), (64, 1500, 900), (128, 1500, 900)])
+def test_results_in_the_place_of_the_queries(c2r, dtype, D, context, window):
+    """Hidden NaN make rows that are computed a second time, from their queries."""
+    rng = np.random.default_rng(59 + D)
+    new, lens = [170, 1, 60], [context + 170, 40, 60]
+    bt = Batch(c2r, rng, dtype, D, 2, 16, lens, new, junk=float("nan"))
+    k, v = (x.clone() for x in bt.rows[0])
+    k[context + 90:context + 100], v[context + 90:context + 100] = float("nan"), float("nan")
+    bt.write(0, k, v)
+    q = _randn(rng, 231, 6, D, dtype=dtype)
+    want = c2r.attention_prefill(q, bt.cache, bt.q_start, 170, None, window, 4)
+    assert torch.isfinite(want[:90]).all()
+    here = q.clone()
+    assert c2r.attention_prefill(here, bt.cache, bt.q_start, 170, None, window, 4, out=here) is here
+    assert torch.equal(here.nan_to_num(7.0), want.nan_to_num(7.0))
+    last = q[(bt.q_start[1:] - 1).long()].contiguous()
+    want = c2r.attention_decode(last, bt.cache, None, window, 4)
+    c2r.attention_decode(last, bt.cache, None, window, 4, out=last)
+    assert torch.equal(last.nan_to_num(7.0), want.nan_to_num(7.0))
