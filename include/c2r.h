@@ -446,7 +446,7 @@ int c2r_distinct_devices(const int32_t *topk_idx, int64_t T, int K, int E, const
  * Limits (else C2R_ERR_UNSUPPORTED): head_dim 64 or 128; up to 1024 heads; batch, pages and tokens below 2^30, page_size *
  * max_pages below 2^28, batch * heads of a decoding step below 2^24, T * heads + 64 * batch * kv_heads of a call for prompts below
  * 2^29 (some larger ones pass).  C2R_ERR_INVALID_ARG: query heads not a multiple of kv_heads, rows or strides that are not whole
- * 16-byte pieces, strides shorter than a row.
+ * 16-byte pieces, strides shorter than a row (of the cache: where it is written; rows that share a place may be read).
  */
 typedef struct {
     int64_t n_pages, page_size, max_pages, batch, kv_heads, head_dim, dtype, page_stride, slot_stride, head_stride;

@@ -127,6 +127,9 @@ extern "C" int c2r_qk_norm_rope_append(const void *q, int64_t q_stride, const vo
     if (rc != C2R_OK) return rc;
     if (T == 0) return C2R_OK;
     if (!q_start && T != cache->batch) return C2R_ERR_INVALID_ARG;
+    // two rows of the cache in one place would be written in any order (reading them is harmless)
+    if ((cache->page_size > 1 && cache->slot_stride < D) || (kv_heads > 1 && cache->head_stride < D) || (cache->n_pages > 1 && cache->page_stride < D))
+        return C2R_ERR_INVALID_ARG;
     const int size = dt == C2R_BF16 ? 2 : 4;
     const int64_t wq = (int64_t)heads * D, wk = (int64_t)kv_heads * D;
     if (!rows_ok(q, q_stride, wq, size) || !rows_ok(k, k_stride, wk, size) || !rows_ok(v, v_stride, wk, size) || !rows_ok(q_out, q_out_stride, wq, size))
