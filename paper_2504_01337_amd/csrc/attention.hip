@@ -181,10 +181,10 @@ static int64_t longest(const c2r_kv_cache *cache, int64_t max_kv_len) {
 }
 
 // Parts that the keys of a bf16 prompt are cut into: the number whose estimated time is least.  Blocks of 128 rows look at up to
-// `tiles` tiles, those of a prompt's first rows at fewer; a block with more than tiles / n is cut.  A tile takes 1.6 us in a
-// block's hands where two blocks share a CU (heads of 128); the call takes as long as its longest part, or as the tiles over the
-// GPU's 512 places and some of a part behind them.  A cut costs a second launch and the writing and reading of the cut rows'
-// sums.  Measured, us, 1 to 4 parts (16 heads unless said): 2000 tokens 51, 46, 42, 57; 1000 behind 16000 361, 208, 182, 160; 500
+// `tiles` tiles, those of a prompt's first rows at fewer; a block with more than tiles / n is cut.  The call takes as long as its
+// longest part, or as the tiles over the GPU's 512 places and some of a part behind them.  A cut costs a second launch and the writing and
+// reading of the cut rows' sums.  A tile (heads of 128) takes 1.6 us where a block has a CU to itself and 2.2 where two share it; the
+// estimate has 1.6 for both and its other constants fitted to the calls measured.  Measured, us, 1 to 4 parts (16 heads unless said): 2000 tokens 51, 46, 42, 57; 1000 behind 16000 361, 208, 182, 160; 500
 // behind 2000, 32 heads 53, 48, 46, 43; three ragged chunks of 700 behind 5000 135, 94, 77, 91; but 4 x 2048 88, 138, 141, 198 and
 // 4000 tokens 96, 115, 106, 135; 256 behind 8000 in 8 parts 41 and whole 174.  Over 24 such calls the choice is 4 % over the best of
 // 1, 2, 3, 4, 6 and 8 parts on average, and 19 % at most (a ragged batch, whose lengths the host does not know).
@@ -196,8 +196,11 @@ static int64_t prompt_parts(const AttnCall &a, int64_t blocks, int64_t tiles, in
     constexpr int SAMPLES = 8;
     int64_t best = 1;
     double least = 0.0;
-    for (int64_t n = 1; n == 1 || (n * units <= ATTN_TILE_BLOCKS && n <= ceil_div(tiles, ATTN_TILE_TILES)); ++n) {
-        const double each = (double)ceil_div(tiles, n);
+    // (numbers of parts of one length are one: 8 tokens behind 200000 keys, one head: 108 estimates and 3 us of the
+    // host's time for 782 and 18)
+    for (int64_t n = 1, length; n == 1 || (n * units <= ATTN_TILE_BLOCKS && n <= ceil_div(tiles, ATTN_TILE_TILES)); n = ceil_div(tiles, length - 1)) {
+        length = ceil_div(tiles, n);
+        const double each = (double)length;
         double all = 0.0, cut = 0.0;  // a block's tiles; its parts, where it is cut
         for (int i = 0; i < SAMPLES; ++i) {
             const double c = fewest + (tiles - fewest) * (i + 0.5) / SAMPLES;
@@ -207,6 +210,7 @@ static int64_t prompt_parts(const AttnCall &a, int64_t blocks, int64_t tiles, in
         const double part = each * rate, spread = 0.9 * units * all * rate / ATTN_TILE_BLOCKS + 0.4 * part;
         const double t = (part > spread ? part : spread) + (n == 1 ? 0.0 : 5.0 + rows * cut * D * 8 / 2e6);
         if (n == 1 || t < least) least = t, best = n;
+        if (length <= 1) break;
     }
     return best;
 }
