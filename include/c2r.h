@@ -506,8 +506,7 @@ int c2r_attention_decode(const void *q, int64_t q_stride, int heads, const c2r_k
  * q_start[b+1] - 1; the last one stands at p = kv_len[b] - 1, the others before it, and their own keys are in the cache
  * already (c2r_qk_norm_rope_append).  A token at p < 0 sees nothing: zeros.
  * T          : rows of q and out;  q_start as in c2r_qk_norm_rope_append, not NULL; rows of no sequence are untouched
- * max_q_len  : host; at least the most new tokens of a sequence: rows past that many are untouched.  The workspace query
- *              covers T up to batch * max_q_len
+ * max_q_len  : host; at least the most new tokens of a sequence: rows past that many are untouched
  * ws         : c2r_workspace_bytes(C2R_STAGE_ATTENTION, T, head_dim, heads, kv_heads, max_q_len, dtype) bytes, 256-aligned
  * Everything else as c2r_attention_decode, but bf16's weights are rounded to bf16 on their way to the second product.
  */

@@ -532,7 +532,7 @@ def attention_prefill(q, cache, q_start, max_q_len, scale=None, window=0, sinks=
     dt = cache.dtype
     assert D == cache.head_dim
     out = torch.empty((T, H, D), dtype=dt, device=q.device) if out is None else out
-    at, n, ws = _attention_ws(T, H, cache, max_q_len, q.device, ws)
+    at, n, ws = _attention_ws(T, H, cache, min(max_q_len, T), q.device, ws)
     _check("c2r_attention_prefill", lib().c2r_attention_prefill(
         *_rows(q, T, H, D, dt), T, H, _vec(q_start, torch.int32, cache.batch + 1), max_q_len, cache.args, max_kv_len,
         D ** -0.5 if scale is None else scale, window, sinks, *_rows(out, T, H, D, dt), at, n, _raw_stream()))

@@ -227,3 +227,13 @@ def test_a_nan_stays_in_its_head(c2r, dtype):
     bad[3, 2] = True                                          # infinity times 0
     assert torch.isnan(qo[3, 2]).any() and torch.isfinite(qo[~bad]).all()
     assert not qo[0].any() and not qo[2].any() and qo[1, 1].any() and qo[4, 1].any()
+
+
+@pytest.mark.parametrize("most", [1 << 20, 1 << 31, (1 << 32) + 1, 1 << 62])
+def test_a_most_that_is_past_every_length(c2r, most):
+    """max_q_len as no limit: the workspace is the one of all T rows."""
+    rng = np.random.default_rng(67)
+    bt = Batch(c2r, rng, "bf16", 128, 16, 16, [1100], [1100])
+    q = _randn(rng, 1100, 16, 128, dtype="bf16")
+    want = _cut(c2r, c2r.attention_prefill, q, bt.cache, bt.q_start, 1100, max_kv_len=1100)
+    assert torch.equal(c2r.attention_prefill(q, bt.cache, bt.q_start, most, max_kv_len=1100), want)
