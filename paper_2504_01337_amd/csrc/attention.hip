@@ -270,8 +270,9 @@ extern "C" int c2r_attention_prefill(const void *q, int64_t q_stride, int64_t T,
     a.row_blocks = (int)(a.by_rows ? by_rows : each);
     const int64_t tiles = attn_max_tiles(a, bf16 ? 64 : 16, ceil_div(per_block, a.group) + 1, longest(cache, max_kv_len));
     // Full precision: parts of 6 tiles (96 keys) or more until there are 1024 blocks.  us, parts of 4, 6, 8 tiles: 512 tokens, 4 heads
-    // of 64 15.8, 16.9, 18.0, 2 x 64 behind 4000 21.8, 20.6, 20.5, 3 x 5 behind 3000 24.6, 22.7, 25.7;  512, 1024, 2048 blocks: 2 x
-    // 2000 tokens, 4 heads of 128 192, 159, 175, 1500 tokens, 8 heads of 64 64, 58, 63.
+    // of 64 14.6, 15.5, 17.0; 2 x 64 behind 4000 21.6, 23.1, 19.8; 3 x 5 behind 3000 23.1, 19.8, 22.8.  512, 1024, 2048 blocks: 1500
+    // tokens, 8 heads of 64 59, 55, 63; 8 ragged of up to 512 44, 52, 52; 2 ragged of up to 2000, 4 heads of 128 184, 191, 165; 400 behind
+    // 6000, 8 heads 164, 177, 153: none is ahead everywhere.
     int64_t parts = bf16 ? prompt_parts(a, blocks, tiles, longest(cache, max_kv_len), (int)cache->head_dim) : attn_parts(blocks, tiles, ATTN_ROWS_BLOCKS, ATTN_ROWS_TILES);
     // (partial results are laid out by rows of q: rows that no sequence has, or past its max_q_len, take their room, too, and
     // more parts than the workspace query foresees are not made)

@@ -1,8 +1,8 @@
 // Attention of one new token per sequence.  The rows of a block are the query heads of one sequence that share a key head (16
 // columns of a product at most; a group of 1 leaves 15 idle, the matrix pipe has the time).  Bound by memory: K and V of the
 // visible keys are read once, and nothing is shared but by these rows.  A block's four waves take the tiles of its part of the
-// keys in turn and add their sums up through LDS.  Heads of 128, bf16: 131 ragged sequences of up to 8000 keys, 32 / 8 heads 371 us with
-// the join (5.6 TB/s; a plain read reaches 6.25); 16 of up to 1500, 32 heads 46 us (4.5); one of 4096, 16 heads 13 us, of which 9 here.
+// keys in turn and add their sums up through LDS.  Heads of 128, bf16: 131 ragged sequences of up to 8000 keys, 32 / 8 heads 374 us with
+// the join (5.5 TB/s; a plain read reaches 6.25); 16 of up to 1500, 32 heads 46 us (4.5); one of 4096, 16 heads 13 us, of which 10 here.
 // Three blocks on a CU: with two, or with K and V through LDS, fewer loads are in flight.
 #include "attn_stream.h"
 

@@ -1,7 +1,7 @@
 // Attention of prompts in full precision: a wave has 16 (token, head of the group) rows, token slowest, the four waves of a
 // block neighbouring ones, so that a tile that one wave loads is in the CU's cache for the others.  Bound by the fp32 matrix
 // pipe (v_mfma_f32_16x16x4_f32) in principle; what it reaches is a fifth of it: every wave loads its tiles itself, 16 rows to 16 keys.
-// 2 x 2000 ragged tokens, 4 heads of 128 157 us (35 TFLOP/s of 154); 512 tokens, 4 heads of 64 16 us with the join.
+// 2 x 2000 ragged tokens, 4 heads of 128 191 us (29 TFLOP/s of 154); 512 tokens, 4 heads of 64 15.5 us with the join.
 #include <type_traits>
 
 #include "attn_stream.h"

@@ -9,9 +9,9 @@
 // K and V tiles are copied straight into LDS, the next pair in flight while one is worked on, one barrier per tile; a row's
 // 16-byte pieces are stored at piece ^ key(row) so that neither read meets on a bank.
 //
-// Bound by issue: a tile of 128 rows is 32 products a wave and some 220 vector instructions, and the chip is power limited under
-// both (1.9 GHz).  Heads of 128: one prompt of 8192 tokens, 16 heads 290 us (950 TFLOP/s of visible pairs; the library's product
-// of 8192^3 reaches 1143); 4 prompts of 2048 88 us (780); 16000 tokens through a window of 2048 with 16 sinks 295 to 320 (790 to 860);
+// Bound by issue: a tile of 128 rows is 32 products a wave and some 210 vector instructions, and the chip is power limited under
+// both (1.9 GHz).  Heads of 128: one prompt of 8192 tokens, 16 heads 288 us (950 TFLOP/s of visible pairs; the library's product
+// of 8192^3 reaches 1143); 4 prompts of 2048 86 us (800); 16000 tokens through a window of 2048 with 16 sinks 292 to 314 (800 to 870);
 // heads of 64, 4 x 2048 51 us (670).  128 rows to a block: K and V are read from LDS by four waves, and 64 rows to a wave, with half
 // those reads, need more registers than stay out of the accumulation half (slower).
 #include "attn_common.h"
