@@ -51,7 +51,10 @@ typedef enum {
     C2R_STAGE_PERMUTE = 2,
     C2R_STAGE_EXPERT_FFN = 3,
     C2R_STAGE_DEDUP_DISPATCH = 4, /* pass the number of devices as E */
-    C2R_STAGE_ATTENTION = 5 /* T tokens, d = head_dim, E = query heads, K = key heads, F = max_q_len (0: decode) */
+    C2R_STAGE_ATTENTION = 5, /* T tokens, d = head_dim, E = query heads, K = key heads, F = max_q_len (0: decode) */
+    C2R_STAGE_ATTENTION_SHARED = 6, /* as C2R_STAGE_ATTENTION; F is not looked at */
+    C2R_STAGE_ADAPTERS = 7,         /* T rows, d = d_in, E = adapters, K = rank */
+    C2R_STAGE_LOGPROBS = 8          /* T rows, d = vocabulary, K = alternatives */
 } c2r_stage;
 
 /* Library version (major*10000 + minor*100 + patch). */
@@ -513,6 +516,81 @@ int c2r_attention_decode(const void *q, int64_t q_stride, int heads, const c2r_k
 int c2r_attention_prefill(const void *q, int64_t q_stride, int64_t T, int heads, const int32_t *q_start, int64_t max_q_len,
                           const c2r_kv_cache *cache, int64_t max_kv_len, float scale, int64_t window, int64_t sinks, void *out,
                           int64_t out_stride, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Decoding of a batch in which runs of sequences begin with the same keys (a long prompt that many requests share, several
+ * answers to one prompt; the decoder blocks of Sec. 4.1's models): c2r_attention_decode, with the same result up to its
+ * roundings, but the keys and values of a shared prefix are read once for a run and not once for each of its sequences.
+ * Run i is the sequences shared_start[i] .. shared_start[i+1] - 1 of the batch; their first shared_len[i] keys are the same, and are
+ * read through the page table's row of the first of them (a whole page of a prefix may be the same page for all; what the
+ * other rows name there is not looked at).  Sequences of no run, or of one with shared_len 0, have all their keys to themselves.  A
+ * sequence shorter than its run's prefix sees of it what c2r_attention_decode would let it see.
+ * shared_start   : int32[n_shared + 1] in DEVICE memory, non-decreasing (entries outside 0 .. batch count as those)
+ * shared_len     : int32[n_shared] in DEVICE memory (below 0: 0; past the table's end: all that it has)
+ * n_shared       : below 2^20; 0: c2r_attention_decode
+ * max_shared_len, max_own_len : host; the longest prefix, and the most keys that a sequence has behind its prefix (0: not known).
+ *                  They only steer the split: results hold for any value.
+ * ws             : c2r_workspace_bytes(C2R_STAGE_ATTENTION_SHARED, batch, head_dim, heads, kv_heads, 0, dtype) bytes, 256-aligned
+ * Everything else as c2r_attention_decode; bf16's weights of a prefix that more than 32 rows of a key head look at are rounded to bf16, as
+ * c2r_attention_prefill's are.
+ */
+int c2r_attention_decode_shared(const void *q, int64_t q_stride, int heads, const c2r_kv_cache *cache, const int32_t *shared_start,
+                                const int32_t *shared_len, int64_t n_shared, int64_t max_shared_len, int64_t max_own_len, float scale,
+                                int64_t window, int64_t sinks, void *out, int64_t out_stride, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * The residual's sum and the root-mean-square norm of whole rows (what stands before each half of the decoder blocks of
+ * Sec. 4.1's models), in one pass:
+ *     s[t] = x[t] + residual[t]           rounded to dt (residual null: s = x)
+ *     y[t] = s[t] * rsqrt(mean(s[t]^2) + eps) * weight            (weight null: 1), rounded to dt
+ *     y8[t] = y[t] / scale[t] in e4m3,  scale[t] = max |y[t]| / 448, at least 2^-126     (y before its rounding)
+ * 32-bit arithmetic.  The outputs that are set are written: sum (only with a residual), y, y8 with scale; the results do not
+ * depend on which.  A row with an infinity or a NaN has NaNs.
+ * x, residual, sum, y : [T, d] of dt, the strides count elements from one row to the next; each output may be an input (same stride)
+ * y8     : bytes [T, d], 8-byte aligned rows;  scale : fp32[T];  weight : fp32[d] (16-byte aligned) or NULL
+ * Limits (else C2R_ERR_UNSUPPORTED): d a multiple of 8 up to 32768, T below 2^30.  C2R_ERR_INVALID_ARG: rows that are not
+ * whole 16-byte pieces (y8: 8), strides shorter than a row, sum without residual, y8 without scale, no output.
+ */
+int c2r_add_rms_norm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, c2r_dtype dt, int64_t T, int d,
+                     const float *weight, float eps, void *sum, int64_t sum_stride, void *y, int64_t y_stride, void *y8, int64_t y8_stride,
+                     float *scale, void *stream);
+
+/*
+ * Low-rank adapters of many requests beside a projection that they share (the projections of the decoder blocks of Sec. 4.1's
+ * models): for every row t with an adapter a = adapter[t],
+ *     out[t] = y[t] + scale[a] * B[a] (A[a] x[t])
+ * and out[t] = y[t] for a row without one (adapter[t] outside [0, n_adapters)).  A[a] x[t] is kept in 32 bits (bf16: its product with B[a]
+ * takes 16 of them), the sum is rounded once.  A row's result depends on the row and its adapter alone, up to the last bits
+ * that the number of rows may change.
+ * x       : [T, d_in] of dt, or with x_scale set bytes in e4m3, row t times x_scale[t] (c2r_add_rms_norm's y8 and scale; dt bf16)
+ * adapter : int32[T] in DEVICE memory;  A : [n_adapters, rank, d_in], B : [n_adapters, d_out, rank] of dt
+ * scale   : fp32[n_adapters] or NULL (1);  y, out : [T, d_out] of dt; out may be y (same stride), and rows without an
+ *           adapter are then not touched
+ * ws      : c2r_workspace_bytes(C2R_STAGE_ADAPTERS, T, d_in, n_adapters, rank, 0, dt) bytes, 256-aligned
+ * Limits (else C2R_ERR_UNSUPPORTED): d_in, d_out, rank multiples of 8, rank up to 128, n_adapters up to 1024, T below 2^24, d_in and d_out
+ * up to 2^20.  C2R_ERR_INVALID_ARG: rows that are not whole 16-byte pieces (x in e4m3: 8), strides shorter than a row.
+ */
+int c2r_adapters(const void *x, int64_t x_stride, const float *x_scale, c2r_dtype dt, int64_t T, int d_in, int d_out, const int32_t *adapter,
+                 int n_adapters, int rank, const void *A, const void *B, const float *scale, const void *y, int64_t y_stride, void *out,
+                 int64_t out_stride, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Log probabilities of given tokens, the entropy and the likeliest tokens, from rows of logits l[t, 0 .. V-1] (the answers that
+ * the benchmarks of Sec. 4.2 score):
+ *     logprob[t, g]     = l[t, tokens[t, g]] - lse,  lse = ln sum_v e^l[t, v];  a token outside [0, V): -infinity
+ *     entropy[t]        = - sum_v p_v ln p_v,  p_v = e^(l[t, v] - lse)          (NULL: not wanted)
+ *     top_token[t, i]   = the i-th largest logit's token, equal ones by the lower index; top_logprob[t, i] its log probability
+ * One pass, 32-bit sums.  A logit of -infinity has probability 0, and the type's lowest value is a number like any other.  A row whose largest logit
+ * is infinite (all of it -infinity, say) or that has a NaN has NaN log probabilities and entropy; its top tokens are those of its numbers, and a place that no
+ * number fills gets token -1 and a NaN.
+ * logits : [T, V] of dt, `stride` elements from one row to the next, any alignment of whole elements
+ * tokens : int32[T, n_given];  logprob : fp32[T, n_given];  entropy : fp32[T];  top_token : int32[T, n_top];  top_logprob : fp32[T, n_top]
+ * ws     : c2r_workspace_bytes(C2R_STAGE_LOGPROBS, T, V, 1, n_top, 0, dt) bytes, 256-aligned (0 for many rows)
+ * Limits (else C2R_ERR_UNSUPPORTED): n_top up to 64, n_given up to 1024, V up to 2^24, T below 2^24.  C2R_ERR_INVALID_ARG: n_top > V, nothing wanted,
+ * a stride below V.
+ */
+int c2r_token_logprobs(const void *logits, c2r_dtype dt, int64_t stride, int64_t T, int V, const int32_t *tokens, int n_given, int n_top,
+                       float *logprob, float *entropy, int32_t *top_token, float *top_logprob, void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

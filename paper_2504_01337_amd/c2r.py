@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libc2r_hip.so")
 
 F32, BF16 = 0, 1
 STAGE_COACTIVATION, STAGE_ROUTE, STAGE_PERMUTE, STAGE_EXPERT_FFN, STAGE_DEDUP_DISPATCH, STAGE_ATTENTION = 0, 1, 2, 3, 4, 5
+STAGE_ATTENTION_SHARED, STAGE_ADAPTERS, STAGE_LOGPROBS = 6, 7, 8
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_LAUNCH = 0, -1, -2, -3, -4
 _ERRNAMES = {-1: "C2R_ERR_INVALID_ARG", -2: "C2R_ERR_UNSUPPORTED", -3: "C2R_ERR_WORKSPACE",
              -4: "C2R_ERR_LAUNCH"}
@@ -28,7 +29,8 @@ EXPORTS = ["c2r_version", "c2r_route_chunk", "c2r_workspace_bytes", "c2r_build_c
            "c2r_expert_ffn_gate_up_with_shared", "c2r_expert_ffn_down_with_shared", "c2r_combine", "c2r_layer_forward",
            "c2r_place_experts", "c2r_dedup_dispatch", "c2r_dedup_dispatch_filled", "c2r_combine_partial", "c2r_combine_copies",
            "c2r_collaboration_degree", "c2r_distinct_devices", "c2r_qk_norm_rope", "c2r_qk_norm_rope_append",
-           "c2r_attention_decode", "c2r_attention_prefill"]
+           "c2r_attention_decode", "c2r_attention_prefill", "c2r_attention_decode_shared", "c2r_add_rms_norm", "c2r_adapters",
+           "c2r_token_logprobs"]
 
 
 class C2RError(RuntimeError):
@@ -82,6 +84,10 @@ def lib():
         L.c2r_qk_norm_rope_append.argtypes = [vp, i64, vp, i64, vp, i64, i64, i32, vp, vp, f32, vp, i32, i32, vp, vp, C.c_char_p, vp, i64, vp]
         L.c2r_attention_decode.argtypes = [vp, i64, i32, C.c_char_p, i64, f32, i64, i64, vp, i64, vp, sz, vp]
         L.c2r_attention_prefill.argtypes = [vp, i64, i64, i32, vp, i64, C.c_char_p, i64, f32, i64, i64, vp, i64, vp, sz, vp]
+        L.c2r_attention_decode_shared.argtypes = [vp, i64, i32, C.c_char_p, vp, vp, i64, i64, i64, f32, i64, i64, vp, i64, vp, sz, vp]
+        L.c2r_add_rms_norm.argtypes = [vp, i64, vp, i64, i32, i64, i32, vp, f32, vp, i64, vp, i64, vp, i64, vp, vp]
+        L.c2r_adapters.argtypes = [vp, i64, vp, i32, i64, i32, i32, vp, i32, i32, vp, vp, vp, vp, i64, vp, i64, vp, sz, vp]
+        L.c2r_token_logprobs.argtypes = [vp, i32, i64, i64, i32, vp, i32, i32, vp, vp, vp, vp, vp, sz, vp]
         for name in EXPORTS[3:]:
             getattr(L, name).restype = i32
         _lib = L
@@ -536,6 +542,91 @@ def attention_prefill(q, cache, q_start, max_q_len, scale=None, window=0, sinks=
     _check("c2r_attention_prefill", lib().c2r_attention_prefill(
         *_rows(q, T, H, D, dt), T, H, _vec(q_start, torch.int32, cache.batch + 1), max_q_len, cache.args, max_kv_len,
         D ** -0.5 if scale is None else scale, window, sinks, *_rows(out, T, H, D, dt), at, n, _raw_stream()))
+    return out
+
+
+def attention_decode_shared(q, cache, shared_start, shared_len, scale=None, window=0, sinks=0, max_shared_len=0, max_own_len=0, ws=None,
+                            out=None):
+    """attention_decode of a batch in which the sequences shared_start[i] .. shared_start[i+1]-1 begin with the same shared_len[i] keys
+    (int32, on the device), which are read once for all of them, through the page table's row of the first.  max_shared_len, max_own_len:
+    the longest prefix and the most keys behind one, if the host knows them.  Returns [batch, heads, D]."""
+    B, H, D = q.shape
+    dt, n = cache.dtype, shared_len.shape[0]
+    assert B == cache.batch and D == cache.head_dim
+    out = torch.empty((B, H, D), dtype=dt, device=q.device) if out is None else out
+    if ws is None:
+        ws = torch.empty(lib().c2r_workspace_bytes(STAGE_ATTENTION_SHARED, B, D, H, cache.kv_heads, 0, 0), dtype=torch.uint8, device=q.device)
+    _check("c2r_attention_decode_shared", lib().c2r_attention_decode_shared(
+        *_rows(q, B, H, D, dt), H, cache.args, _vec(shared_start, torch.int32, n + 1), _vec(shared_len, torch.int32, n), n, max_shared_len,
+        max_own_len, D ** -0.5 if scale is None else scale, window, sinks, *_rows(out, B, H, D, dt), ws.data_ptr(), ws.numel(), _raw_stream()))
+    return out
+
+
+def _matrix(t: Optional[torch.Tensor], T, d, dtype):
+    """(address, elements from one row to the next) of rows [T, d], or of none."""
+    if t is None:
+        return None, 0
+    assert t.shape == (T, d) and t.dtype is dtype and t.is_cuda and (t.stride(1) == 1 or d == 1), "device-resident rows [T, d] of one type"
+    return t.data_ptr(), t.stride(0) if T > 1 else -(-d // 8) * 8
+
+
+def add_rms_norm(x, residual=None, weight=None, eps=1e-6, dense=True, bits8=False, out=None):
+    """s = x + residual and its root-mean-square norm over rows [T, d], as rows of x's type (dense), in 8 bits with a scale for
+    each row (bits8: y8 * scale stands for y), or both.  out = (y, sum, y8, scale), each may be None where it is not wanted; y and
+    sum may be inputs.  Returns these four."""
+    T, d = x.shape
+    dt = x.dtype
+    if out is None:
+        out = (torch.empty((T, d), dtype=dt, device=x.device) if dense else None,
+               None if residual is None else torch.empty((T, d), dtype=dt, device=x.device),
+               torch.empty((T, d), dtype=torch.float8_e4m3fn, device=x.device) if bits8 else None,
+               torch.empty((T,), dtype=torch.float32, device=x.device) if bits8 else None)
+    y, total, y8, scale = out
+    _check("c2r_add_rms_norm", lib().c2r_add_rms_norm(
+        *_matrix(x, T, d, dt), *_matrix(residual, T, d, dt), _dt(x), T, d, _vec(weight, torch.float32, d), eps, *_matrix(total, T, d, dt),
+        *_matrix(y, T, d, dt), *_matrix(y8, T, d, torch.float8_e4m3fn), _vec(scale, torch.float32, T), _raw_stream()))
+    return out
+
+
+def adapters(x, adapter, A, B, y, scale=None, x_scale=None, ws=None, out=None):
+    """Low-rank adapters of many requests beside a projection that they share: out[t] = y[t] + scale[a] * B[a] (A[a] x[t]) with
+    a = adapter[t] (int32[T]; outside [0, n): out[t] = y[t]).  A[n, rank, d_in], B[n, d_out, rank]; x[T, d_in] of their type, or in e4m3
+    with x_scale[T] (add_rms_norm's y8 and scale).  out may be y.  Returns out[T, d_out]."""
+    T, d_in = x.shape
+    n, r, _ = A.shape
+    d_out, dt = B.shape[1], A.dtype
+    assert A.shape[2] == d_in and B.shape == (n, d_out, r) and B.dtype is dt
+    out = torch.empty((T, d_out), dtype=dt, device=x.device) if out is None else out
+    if ws is None:
+        ws = torch.empty(max(256, lib().c2r_workspace_bytes(STAGE_ADAPTERS, T, d_in, n, r, 0, 0)), dtype=torch.uint8, device=x.device)
+    _check("c2r_adapters", lib().c2r_adapters(
+        *_matrix(x, T, d_in, dt if x_scale is None else torch.float8_e4m3fn), _vec(x_scale, torch.float32, T), _dt(A), T, d_in, d_out,
+        _vec(adapter, torch.int32, T), n, r, _ptr(A), _ptr(B), _vec(scale, torch.float32, n), *_matrix(y, T, d_out, dt),
+        *_matrix(out, T, d_out, dt), ws.data_ptr(), ws.numel(), _raw_stream()))
+    return out
+
+
+def token_logprobs(logits, tokens=None, n_top=0, entropy=True, ws=None, out=None):
+    """From logits[T, V] the log probabilities of tokens[T, n] (int32; or [T], or None), the entropy and the n_top likeliest tokens with theirs,
+    equal logits by the lower index.  Returns (logprob, entropy, top_token, top_logprob), None what is not asked for."""
+    T, V = logits.shape
+    dev = logits.device
+    assert logits.is_cuda and (V == 1 or logits.stride(1) == 1)
+    given = 0
+    if tokens is not None:
+        assert tokens.dtype is torch.int32 and tokens.is_cuda and tokens.is_contiguous() and tokens.shape[0] == T
+        given = tokens.numel() // T if T else 0
+    if out is None:
+        f32 = dict(dtype=torch.float32, device=dev)
+        out = (torch.empty(tokens.shape, **f32) if given else None, torch.empty((T,), **f32) if entropy else None,
+               torch.empty((T, n_top), dtype=torch.int32, device=dev) if n_top else None, torch.empty((T, n_top), **f32) if n_top else None)
+    lp, ent, top, top_lp = out
+    if ws is None:
+        need = lib().c2r_workspace_bytes(STAGE_LOGPROBS, T, V, 1, n_top, 0, 0)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    _check("c2r_token_logprobs", lib().c2r_token_logprobs(
+        logits.data_ptr(), _dt(logits), logits.stride(0) if T > 1 else V, T, V, _addr(tokens), given, n_top, _addr(lp), _addr(ent), _addr(top),
+        _addr(top_lp), 0 if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _raw_stream()))
     return out
 
 

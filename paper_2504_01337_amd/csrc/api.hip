@@ -7,6 +7,9 @@ size_t route_workspace_bytes(int64_t T, int d, int E);
 size_t permute_workspace_bytes(int64_t T, int E, int K);
 size_t dedup_workspace_bytes(int64_t T, int n_dev);
 size_t attention_workspace_bytes(int64_t T, int D, int heads, int kv_heads, int max_q_len);
+size_t attention_shared_workspace_bytes(int64_t T, int D, int heads, int kv_heads);
+size_t adapters_workspace_bytes(int64_t T, int d_in, int E, int r);
+size_t logprobs_workspace_bytes(int64_t T, int V, int n);
 int launch_ffn_f32_pass(int pass, const float *a, const int32_t *offsets, int E_local, int64_t A_cap, int d,
                         int F, const float *b0, const float *b1, float *out, hipStream_t st);
 int launch_ffn_bf16_pass(int pass, const uint16_t *a, const int32_t *offsets, int E_local, int64_t A_cap, int d,
@@ -61,6 +64,12 @@ extern "C" size_t c2r_workspace_bytes(int stage, int64_t T, int d, int E, int K,
             return dedup_workspace_bytes(T, E);  // E: number of devices
         case C2R_STAGE_ATTENTION:
             return attention_workspace_bytes(T, d, E, K, F);  // d: head width, E, K: query and key heads, F: max_q_len
+        case C2R_STAGE_ATTENTION_SHARED:
+            return attention_shared_workspace_bytes(T, d, E, K);
+        case C2R_STAGE_ADAPTERS:
+            return adapters_workspace_bytes(T, d, E, K);  // d: d_in, E: adapters, K: rank
+        case C2R_STAGE_LOGPROBS:
+            return logprobs_workspace_bytes(T, d, K);  // d: vocabulary, K: alternatives
         default:
             return 0;
     }

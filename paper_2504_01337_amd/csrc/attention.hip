@@ -17,11 +17,6 @@ static int check_heads(int dt, int heads, int64_t kv_heads, int64_t D) {
     return D == 64 || D == 128 ? C2R_OK : C2R_ERR_UNSUPPORTED;
 }
 
-// Rows of `width` elements, `stride` apart, that the kernels touch 16 bytes at a time.
-static bool rows_ok(const void *p, int64_t stride, int64_t width, int size) {
-    return p && aligned(p, 16) && stride >= width && stride <= (1ll << 40) && stride * size % 16 == 0;
-}
-
 static int check_cache(const c2r_kv_cache *c, int heads) {
     if (!c) return C2R_ERR_INVALID_ARG;
     if (c->dtype != C2R_F32 && c->dtype != C2R_BF16) return C2R_ERR_INVALID_ARG;
@@ -84,6 +79,14 @@ size_t attention_workspace_bytes(int64_t T, int D, int heads, int kv_heads, int 
         return round_up((size_t)bound(ATTN_DECODE_EVEN_BLOCKS, heads / kv_heads < 16 ? heads / kv_heads : 16) * (size_t)(D + 2) * 4, 256);
     const int64_t tile = bound(ATTN_TILE_BLOCKS, ATTN_TILE_ROWS), full = bound(ATTN_ROWS_BLOCKS, ATTN_ROWS_ROWS);
     return round_up((size_t)(tile > full ? tile : full) * (size_t)(D + 2) * 4, 256);
+}
+
+// The rows x parts of a batch behind shared prefixes: parts of the prefixes, of any of the kernels, and of what lies behind.
+size_t attention_shared_workspace_bytes(int64_t T, int D, int heads, int kv_heads) {
+    if (T <= 0 || D <= 0 || heads <= 0 || kv_heads <= 0) return 0;
+    const int64_t rows = T * heads, prefix = (int64_t)ATTN_TILE_BLOCKS * ATTN_TILE_ROWS, cols = heads / kv_heads < 16 ? heads / kv_heads : 16;
+    static_assert(ATTN_TILE_BLOCKS * ATTN_TILE_ROWS >= ATTN_DECODE_BLOCKS * 16, "either kernel's parts of a prefix");
+    return round_up((size_t)(prefix + rows + ATTN_DECODE_EVEN_BLOCKS * cols + rows) * (size_t)(D + 2) * 4, 256);
 }
 
 }  // namespace c2r
@@ -217,12 +220,23 @@ static int64_t prompt_parts(const AttnCall &a, int64_t blocks, int64_t tiles, in
 
 // Partial results go to the workspace where the keys are cut.
 static int place_parts(AttnCall &a, int D, void *ws, size_t ws_bytes) {
-    if (a.splits == 1) return C2R_OK;
+    if (a.splits == 1 && !a.shared) return C2R_OK;
     const size_t rows = (size_t)a.T * a.heads * a.splits;
     if (!ws || !aligned(ws, 256) || ws_bytes < rows * (size_t)(D + 2) * 4) return C2R_ERR_WORKSPACE;
     a.part_o = static_cast<float *>(ws);
     a.part_ml = a.part_o + rows * D;
     return C2R_OK;
+}
+
+// Few blocks: parts of 8 tiles or more (256 keys in bf16) until the GPU's 768 places are taken.  Many: long sequences in
+// parts of 24 or more, so that a batch of ragged lengths ends evenly.  Microseconds, bf16, heads of 128:
+//   1 x 4096 keys, 16 key heads: parts of 4, 8, 24 tiles 13.5, 13.4, 16;  1 x 32000: parts of 8, 21, 24 57, 52.5, 53
+//   131 ragged sequences of up to 8000, 8 key heads, 1, 2, 3, 5 parts: 393, 420, 376, 371
+//   256 ragged sequences of up to 500, 16 key heads, parts of 8 tiles and whole: 120 and 97
+static int64_t decode_parts(int64_t blocks, int64_t tiles) {
+    const int64_t fill = attn_parts(blocks, tiles, ATTN_DECODE_BLOCKS, ATTN_DECODE_TILES);
+    const int64_t even = attn_parts(blocks, tiles, ATTN_DECODE_EVEN_BLOCKS, ATTN_DECODE_EVEN_TILES);
+    return fill > even ? fill : even;
 }
 
 extern "C" int c2r_attention_decode(const void *q, int64_t q_stride, int heads, const c2r_kv_cache *cache, int64_t max_kv_len, float scale,
@@ -234,15 +248,8 @@ extern "C" int c2r_attention_decode(const void *q, int64_t q_stride, int heads, 
     if (rc != C2R_OK || cache->batch == 0) return rc;
     const bool bf16 = cache->dtype == C2R_BF16;
     const int64_t blocks = cache->batch * cache->kv_heads * ceil_div(a.group, 16);
-    // Few blocks: parts of 8 tiles or more (256 keys in bf16) until the GPU's 768 places are taken.  Many: long sequences in
-    // parts of 24 or more, so that a batch of ragged lengths ends evenly.  Microseconds, bf16, heads of 128:
-    //   1 x 4096 keys, 16 key heads: parts of 4, 8, 24 tiles 13.5, 13.4, 16;  1 x 32000: parts of 8, 21, 24 57, 52.5, 53
-    //   131 ragged sequences of up to 8000, 8 key heads, 1, 2, 3, 5 parts: 393, 420, 376, 371
-    //   256 ragged sequences of up to 500, 16 key heads, parts of 8 tiles and whole: 120 and 97
     const int64_t tiles = attn_max_tiles(a, bf16 ? 32 : 16, 1, longest(cache, max_kv_len));
-    const int64_t fill = attn_parts(blocks, tiles, ATTN_DECODE_BLOCKS, ATTN_DECODE_TILES);
-    const int64_t even = attn_parts(blocks, tiles, ATTN_DECODE_EVEN_BLOCKS, ATTN_DECODE_EVEN_TILES);
-    attn_split(a, tiles, fill > even ? fill : even);
+    attn_split(a, tiles, decode_parts(blocks, tiles));
     if (blocks * a.splits >= ATTN_MOST_BLOCKS) return C2R_ERR_UNSUPPORTED;
     rc = place_parts(a, (int)cache->head_dim, ws, ws_bytes);
     return rc == C2R_OK ? launch_attn_decode(a, bf16, (int)cache->head_dim, static_cast<hipStream_t>(stream)) : rc;
@@ -285,4 +292,43 @@ extern "C" int c2r_attention_prefill(const void *q, int64_t q_stride, int64_t T,
     if (rc != C2R_OK) return rc;
     return bf16 ? launch_attn_tile(a, (int)cache->head_dim, static_cast<hipStream_t>(stream))
                 : launch_attn_rows_f32(a, (int)cache->head_dim, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int c2r_attention_decode_shared(const void *q, int64_t q_stride, int heads, const c2r_kv_cache *cache, const int32_t *shared_start,
+                                           const int32_t *shared_len, int64_t n_shared, int64_t max_shared_len, int64_t max_own_len, float scale,
+                                           int64_t window, int64_t sinks, void *out, int64_t out_stride, void *ws, size_t ws_bytes, void *stream) {
+    drop_stale_error();
+    if (!cache || n_shared < 0) return C2R_ERR_INVALID_ARG;
+    AttnCall a;
+    int rc = attention_call(q, q_stride, cache->batch, heads, cache, scale, window, sinks, out, out_stride, a);
+    if (rc != C2R_OK || cache->batch == 0) return rc;
+    if (n_shared >= ATTN_MOST_RUNS) return C2R_ERR_UNSUPPORTED;
+    if (n_shared == 0) return c2r_attention_decode(q, q_stride, heads, cache, max_own_len, scale, window, sinks, out, out_stride, ws, ws_bytes, stream);
+    if (!shared_start || !shared_len || !aligned(shared_start, 4) || !aligned(shared_len, 4)) return C2R_ERR_INVALID_ARG;
+    const bool bf16 = cache->dtype == C2R_BF16;
+    const int D = (int)cache->head_dim;
+    if (cache->batch * a.group >= (1ll << 30)) return C2R_ERR_UNSUPPORTED;
+    a.shared_start = shared_start, a.shared_len = shared_len, a.shared = (int)n_shared;
+    // the prefixes
+    const bool tiled = bf16 && cache->batch * a.group > ATTN_PREFIX_ROWS * n_shared;
+    const int64_t per_block = tiled ? ATTN_TILE_ROWS : 16, KT = tiled ? 64 : bf16 ? 32 : 16;
+    const int64_t rows = cache->batch * a.group / per_block + n_shared, prefix_tiles = ceil_div(longest(cache, max_shared_len), KT);
+    int64_t parts = attn_parts(rows * cache->kv_heads, prefix_tiles, tiled ? ATTN_TILE_BLOCKS : ATTN_DECODE_BLOCKS, tiled ? ATTN_TILE_TILES : ATTN_DECODE_TILES);
+    a.prefix_tiles = (int)ceil_div(prefix_tiles, parts);
+    a.prefix_splits = (int)ceil_div(prefix_tiles, a.prefix_tiles);
+    a.prefix_blocks = (int)rows;
+    // what lies behind them
+    const int64_t blocks = cache->batch * cache->kv_heads * ceil_div(a.group, 16);
+    const int64_t tiles = attn_max_tiles(a, bf16 ? 32 : 16, 1, longest(cache, max_own_len));
+    attn_split(a, tiles, decode_parts(blocks, tiles));
+    if (rows * cache->kv_heads * a.prefix_splits + blocks * a.splits >= ATTN_MOST_BLOCKS) return C2R_ERR_UNSUPPORTED;
+    a.splits += a.prefix_splits;
+    rc = place_parts(a, D, ws, ws_bytes);
+    if (rc != C2R_OK) return rc;
+    if (tiled) {
+        rc = launch_attn_tile_prefix(a, D, static_cast<hipStream_t>(stream));
+        if (rc != C2R_OK) return rc;
+        a.prefix_blocks = 0;
+    }
+    return launch_attn_shared(a, bf16, D, static_cast<hipStream_t>(stream));
 }

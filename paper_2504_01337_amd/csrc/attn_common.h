@@ -54,6 +54,11 @@ __device__ __forceinline__ int count_first(int n, const F &below) {
 // first part, which has written the result.
 constexpr float PART_EMPTY = -1.0f, PART_DONE = -2.0f;
 
+// Keys of a sequence that a block looks at, of those its queries see: all of them, a prefix, or what lies behind one.
+struct KeyRange {
+    int from = 0, to = 0x7fffffff;
+};
+
 // One call of attention.  New tokens of sequence b: rows q_start[b] .. of q (b .. b + 1 where q_start is null); the last of
 // them stands at position kv_len[b] - 1.
 struct AttnCall {
@@ -73,6 +78,11 @@ struct AttnCall {
     // else as many for each sequence as max_q needs.
     int row_blocks;
     bool by_rows;
+    // Runs of sequences that begin with the same keys: run i is the sequences shared_start[i] .. shared_start[i + 1] - 1, its keys the
+    // first shared_len[i] of the first of them.  The first prefix_splits of the parts are cut from these, after every
+    // prefix_tiles tiles, the others from the sequences' own keys.  prefix_blocks: rows of blocks that the prefixes have.
+    const int32_t *shared_start, *shared_len;
+    int shared, prefix_splits, prefix_tiles, prefix_blocks;
     float *part_o, *part_ml;  // [splits][T * heads][D] sums, [splits][T * heads][2] maximum and denominator (or PART_..)
 
     __device__ __forceinline__ int first_row(int b) const { return q_start ? (int)clamp_row(q_start[b]) : b; }
@@ -99,10 +109,29 @@ struct AttnCall {
         rb = (int)((rows + BM - 1) / BM) - 1 - (x - begin(b));
         return rb >= 0;
     }
-    // The last key that is cached of those up to position p.
+    __device__ __forceinline__ int shared_first(int i) const { return (int)clamp_row(shared_start[i]); }
+    __device__ __forceinline__ int shared_keys(int i) const { return min(max(shared_len[i], 0), kv.capacity); }
+    // The run that sequence b is in, -1: none.
+    __device__ __forceinline__ int run_of(int b) const {
+        const int i = count_first(shared, [&](int r) { return shared_first(r) <= b; }) - 1;
+        return i >= 0 && b < shared_first(i + 1) ? i : -1;
+    }
+    // Block x of a key head's and part's: run i and block rb of its (sequence, head of the group) rows, counted as in block_of.
+    template <int BM>
+    __device__ __forceinline__ bool prefix_block_of(int x, int &i, int &rb, int &rows) const {
+        auto begin = [&](int r) { return (int)((int64_t)shared_first(r) * group / BM) + r; };
+        i = count_first(shared, [&](int r) { return begin(r) <= x; }) - 1;
+        if (i < 0) return false;
+        rows = (shared_first(i + 1) - shared_first(i)) * group;
+        rb = x - begin(i);
+        return rb * BM < rows && shared_keys(i) > 0;
+    }
+    // The last key that is cached of those up to position p, and of those the last one of keys[.., to).
     __device__ __forceinline__ int last_key(int p) const { return min(p, kv.capacity - 1); }
+    __device__ __forceinline__ int last_key(int p, KeyRange keys) const { return min(last_key(p), keys.to - 1); }
     // Whether the query at position p sees key j; whether it sees none.
     __device__ __forceinline__ bool sees(int p, int j) const { return j <= last_key(p) && (!window || j > p - window || j < sinks); }
+    __device__ __forceinline__ bool sees(int p, int j, KeyRange keys) const { return j >= keys.from && j < keys.to && sees(p, j); }
     __device__ __forceinline__ bool blind(int p) const { return p < 0 || (window && !sinks && p - window >= kv.capacity - 1); }
 };
 
@@ -110,24 +139,30 @@ struct AttnCall {
 // before the window, then the window's.
 template <int KT>
 struct KeyTiles {
-    int sink_tiles, first, count;
-    __device__ __forceinline__ KeyTiles(const AttnCall &a, int p_min, int p_max) {
-        sink_tiles = first = 0;
+    int sink_tiles, first, count, skipped;  // skipped: tiles before the range's first
+    __device__ __forceinline__ KeyTiles(const AttnCall &a, int p_min, int p_max, KeyRange keys = KeyRange()) {
+        skipped = keys.from / KT;
+        const int last = a.last_key(p_max, keys);  // (a window that begins past the cache's end leaves the sinks)
+        sink_tiles = 0, first = skipped;
         if (a.window) {
             const int lo = p_min - a.window + 1;
-            first = lo > 0 ? lo / KT : 0;
-            const int s = (int)(((int64_t)a.sinks + KT - 1) / KT);
-            sink_tiles = s < first ? s : first;
+            first = lo > keys.from ? lo / KT : skipped;
+            // (sinks past the range's end are no tiles of it)
+            int s = (int)(((int64_t)a.sinks + KT - 1) / KT);
+            if (keys.to != 0x7fffffff) s = min(s, last < 0 ? 0 : last / KT + 1);
+            sink_tiles = max((s < first ? s : first) - skipped, 0);
         }
-        const int last = a.last_key(p_max);  // (a window that begins past the cache's end leaves the sinks)
-        count = last < 0 ? 0 : sink_tiles + max(last / KT - first + 1, 0);
+        count = last < keys.from ? 0 : sink_tiles + max(last / KT - first + 1, 0);
     }
-    __device__ __forceinline__ int base(int x) const { return (x < sink_tiles ? x : first + x - sink_tiles) * KT; }
-    // [x0, x1): the part of split s.  The last one takes what is left, however long a sequence is.
-    __device__ __forceinline__ void part(const AttnCall &a, int s, int &x0, int &x1) const {
-        const int64_t lo = (int64_t)s * a.split_tiles, hi = s + 1 == a.splits ? count : lo + a.split_tiles;
+    __device__ __forceinline__ int base(int x) const { return (x < sink_tiles ? skipped + x : first + x - sink_tiles) * KT; }
+    __device__ __forceinline__ void part(int n, int tiles, int s, int &x0, int &x1) const {
+        const int64_t lo = (int64_t)s * tiles, hi = s + 1 == n ? count : lo + tiles;
         x0 = lo < count ? (int)lo : count;
         x1 = hi < count ? (int)hi : count;
+    }
+    // [x0, x1): the part of split s.  The last one takes what is left, however long a sequence is.
+    __device__ __forceinline__ void part(const AttnCall &a, int s, int &x0, int &x1) const {
+        part(a.splits, a.split_tiles, s, x0, x1);
     }
     // Whether split 0 has all of them: it then writes the result itself and says so to the join (PART_DONE).
     __device__ __forceinline__ bool uncut(const AttnCall &a) const { return a.splits == 1 || count <= a.split_tiles; }
@@ -135,8 +170,8 @@ struct KeyTiles {
 
 // A tile [base, base + KT) that every query of p_min .. p_max sees whole.
 template <int KT>
-__device__ __forceinline__ bool tile_whole(const AttnCall &a, int base, int p_min, int p_max) {
-    return base + KT - 1 <= a.last_key(p_min) && (!a.window || base > p_max - a.window || base + KT <= a.sinks);
+__device__ __forceinline__ bool tile_whole(const AttnCall &a, int base, int p_min, int p_max, KeyRange keys = KeyRange()) {
+    return base >= keys.from && base + KT - 1 <= a.last_key(p_min, keys) && (!a.window || base > p_max - a.window || base + KT <= a.sinks);
 }
 
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
@@ -155,7 +190,8 @@ __device__ __forceinline__ float load_element(const unsigned char *p, int i) {
 // that finite inputs pay one check per output.  The whole wave runs it: a lane holds a key's score, then D / 64 elements.
 template <bool BF16, int D, int KT>
 __device__ __forceinline__ void exact_row(const AttnCall &a, const KeyTiles<KT> tiles, int x0, int x1, int step, int b, int kv_head,
-                                          int p, const unsigned char *q_row, float &m_out, float &l_out, float (&o)[D / 64]) {
+                                          int p, const unsigned char *q_row, float &m_out, float &l_out, float (&o)[D / 64],
+                                          KeyRange keys = KeyRange()) {
     constexpr int N = D / 64;
     const int lane = lane_id();
     float m = -__builtin_inff(), l = 0.0f;
@@ -163,7 +199,7 @@ __device__ __forceinline__ void exact_row(const AttnCall &a, const KeyTiles<KT> 
     for (int i = 0; i < N; ++i) o[i] = 0.0f;
     for (int x = x0; x < x1; x += step) {
         const int j = tiles.base(x) + lane;
-        const bool see = lane < KT && a.sees(p, j);
+        const bool see = lane < KT && a.sees(p, j, keys);
         int64_t at = 0;
         float s = -__builtin_inff();
         if (see) {
@@ -214,6 +250,10 @@ int launch_qk_norm_rope(RopeCall a, bool bf16, int D, bool neighbours, hipStream
 int launch_attn_join(const AttnCall &a, bool bf16, int D, hipStream_t st);
 // attn_decode.hip: one new token per sequence.
 int launch_attn_decode(const AttnCall &a, bool bf16, int D, hipStream_t st);
+// attn_shared.hip: one new token per sequence behind prefixes that runs of sequences share.
+int launch_attn_shared(const AttnCall &a, bool bf16, int D, hipStream_t st);
+// attn_tile.hip: the parts of a shared prefix, bf16.
+int launch_attn_tile_prefix(const AttnCall &a, int D, hipStream_t st);
 // attn_rows.hip: prompts in full precision.
 int launch_attn_rows_f32(const AttnCall &a, int D, hipStream_t st);
 // attn_tile.hip: prompts in bf16, key tiles through LDS.
@@ -233,6 +273,10 @@ constexpr int ATTN_ROWS_BLOCKS = 1024, ATTN_ROWS_TILES = 6, ATTN_ROWS_ROWS = 64;
 constexpr int ATTN_BY_ROWS = 2;
 // Blocks of a join from which on keys are not cut: nearly all of them would find nothing to do.
 constexpr int64_t ATTN_JOIN_BLOCKS = 1 << 17;
+
+// Rows of a shared prefix, per key head, from which on its keys go through LDS.
+constexpr int ATTN_PREFIX_ROWS = 32;
+constexpr int64_t ATTN_MOST_RUNS = 1 << 20;
 
 // A grid's threads are counted in 32 bits.
 constexpr int64_t ATTN_MOST_BLOCKS = 1ll << 24;

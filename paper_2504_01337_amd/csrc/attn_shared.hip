@@ -1,0 +1,126 @@
+// Attention of one new token per sequence where runs of sequences begin with the same keys: those are read once for a run, as far as 16
+// rows go, and not once for a sequence.  The rows of a block are either (sequence, query head) pairs of one run and one key head, against
+// a part of the run's keys, or the query heads of one sequence that share a key head, against a part of the keys behind.  All
+// results are partial, and joined.  Few rows to a run, or full precision: prefixes in bf16 that many rows look at go
+// through LDS (attn_tile.hip), and this kernel has the keys behind them.  Bound by memory.
+#include "attn_stream.h"
+
+namespace c2r {
+
+template <bool BF16, int D>
+__global__ __launch_bounds__(256, D == 128 ? 3 : 4) void attn_shared_kernel(AttnCall a, uint32_t prefix_grid) {
+    using S = Stream<BF16, D>;
+    constexpr int SZ = S::SZ, KT = S::KT;
+    __shared__ __align__(16) float join_o[4 * 16 * D], join_ml[4 * 16 * 2];
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, n = lane & 15;
+    // blocks: those of the prefixes, then those of the sequences; parts of the keys fastest, then key heads, rows
+    int b, kv_head, row0, left, part, splits, split_tiles;
+    KeyRange keys;
+    uint32_t id = blockIdx.x;
+    const bool prefix = id < prefix_grid;
+    if (prefix) {
+        splits = a.prefix_splits, split_tiles = a.prefix_tiles;
+        part = (int)(id % splits);
+        id /= splits;
+        kv_head = (int)(id % a.kv.kv_heads);
+        int run, rb, rows;
+        if (!a.prefix_block_of<16>((int)(id / a.kv.kv_heads), run, rb, rows)) return;
+        b = a.shared_first(run), keys.to = a.shared_keys(run);
+        row0 = rb * 16, left = min(rows - row0, 16);
+    } else {
+        id -= prefix_grid;
+        splits = a.splits - a.prefix_splits, split_tiles = a.split_tiles;
+        part = (int)(id % splits);
+        id /= splits;
+        const int col_sets = (a.group + 15) / 16;
+        row0 = (int)(id % col_sets) * 16, left = min(a.group - row0, 16);
+        id /= col_sets;
+        kv_head = (int)(id % a.kv.kv_heads);
+        b = (int)(id / a.kv.kv_heads);
+        const int run = a.run_of(b);
+        keys.from = run < 0 ? 0 : a.shared_keys(run);
+    }
+    // row r: a sequence and a head
+    auto sequence = [&](int r) { return b + r / a.group; };
+    auto head_of = [&](int r) { return kv_head * a.group + r % a.group; };
+    auto place = [&](int r, int in) { return ((int64_t)in * a.kv.batch + sequence(r)) * a.heads + head_of(r); };
+    auto put_empty = [&](int r, int in) {
+        float *ml = a.part_ml + place(r, in) * 2;
+        ml[0] = -__builtin_inff(), ml[1] = PART_EMPTY;
+    };
+    if (!prefix && part == 0 && keys.from == 0)  // (no block has a prefix of these)
+        for (int i = threadIdx.x; i < left * a.prefix_splits; i += 256) put_empty(row0 + i % left, i / left);
+    const int here = part + (prefix ? 0 : a.prefix_splits);
+    const int row = row0 + min(n, left - 1), p = a.kv.tokens(sequence(row)) - 1;
+    int p_min = p, p_max = p;
+#pragma unroll
+    for (int w = 8; w; w >>= 1) p_min = min(p_min, __shfl_xor(p_min, w)), p_max = max(p_max, __shfl_xor(p_max, w));
+    p_min = __builtin_amdgcn_readfirstlane(p_min), p_max = __builtin_amdgcn_readfirstlane(p_max);
+    const KeyTiles<KT> tiles(a, p_min, p_max, keys);
+    int x0, x1;
+    tiles.part(splits, split_tiles, part, x0, x1);
+    if (x0 == x1) {
+        if (threadIdx.x < (uint32_t)left) put_empty(row0 + threadIdx.x, here);
+        return;
+    }
+    auto q_row = [&](int r) { return a.q + sequence(r) * a.q_bytes + (int64_t)head_of(r) * (D * SZ); };
+    u32x4 q[S::KSTEPS];
+    const unsigned char *mine_q = q_row(row);
+#pragma unroll
+    for (int c = 0; c < S::KSTEPS; ++c) q[c] = *reinterpret_cast<const u32x4 *>(mine_q + c * 64 + g * 16);
+    typename S::State st;
+    S::clear(st);
+    S::template run<4>(a, q, st, tiles, x0 + wave, x1, b, kv_head * a.kv.head_bytes, p, p_min, p_max, keys);
+    uint32_t redo = S::finish(st, left);
+    float *mine = join_o + wave * 16 * D;
+    if (n < left && !(redo >> n & 1)) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < S::VEL; ++e) mine[n * D + (g * 4 + r) * S::VEL + e] = st.o[e][r];
+        if (g == 0) join_ml[(wave * 16 + n) * 2] = st.m, join_ml[(wave * 16 + n) * 2 + 1] = st.l;
+    }
+    while (redo) {
+        const int col = __ffs(redo) - 1;
+        redo &= redo - 1;
+        float m, l, o[D / 64];
+        exact_row<BF16, D, KT>(a, tiles, x0 + wave, x1, 4, b, kv_head, a.kv.tokens(sequence(row0 + col)) - 1, q_row(row0 + col), m, l, o, keys);
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) mine[col * D + lane * (D / 64) + e] = o[e];
+        if (lane == 0) join_ml[(wave * 16 + col) * 2] = m, join_ml[(wave * 16 + col) * 2 + 1] = l;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < left * (D / 4); i += 256) {
+        const int col = i / (D / 4), d = i % (D / 4) * 4;
+        float m4[4], M = -__builtin_inff(), l = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) m4[w] = join_ml[(w * 16 + col) * 2], M = fmaxf(M, m4[w]);
+        const float ref = reference_of(M);
+        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = __builtin_amdgcn_exp2f(m4[w] - ref);
+            l = __builtin_fmaf(f, join_ml[(w * 16 + col) * 2 + 1], l);
+            const f32x4 o = *reinterpret_cast<const f32x4 *>(join_o + (w * 16 + col) * D + d);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] = __builtin_fmaf(f, o[e], sum[e]);
+        }
+        const int64_t at = place(row0 + col, here);
+        *reinterpret_cast<f32x4 *>(a.part_o + at * D + d) = sum;
+        if (d == 0) a.part_ml[at * 2] = M, a.part_ml[at * 2 + 1] = a.blind(a.kv.tokens(sequence(row0 + col)) - 1) ? PART_EMPTY : l;
+    }
+}
+
+int launch_attn_shared(const AttnCall &a, bool bf16, int D, hipStream_t st) {
+    // (prefix_blocks 0: their parts are another kernel's)
+    const uint32_t prefix = (uint32_t)((int64_t)a.prefix_blocks * a.kv.kv_heads * a.prefix_splits);
+    const dim3 grid(prefix + (unsigned)((int64_t)(a.splits - a.prefix_splits) * a.kv.kv_heads * ((a.group + 15) / 16) * a.kv.batch)), block(256);
+    if (bf16 && D == 128) attn_shared_kernel<true, 128><<<grid, block, 0, st>>>(a, prefix);
+    else if (bf16) attn_shared_kernel<true, 64><<<grid, block, 0, st>>>(a, prefix);
+    else if (D == 128) attn_shared_kernel<false, 128><<<grid, block, 0, st>>>(a, prefix);
+    else attn_shared_kernel<false, 64><<<grid, block, 0, st>>>(a, prefix);
+    const int rc = launch_status();
+    return rc == C2R_OK ? launch_attn_join(a, bf16, D, st) : rc;
+}
+
+}  // namespace c2r

@@ -103,7 +103,7 @@ struct Stream {
 
     // Scores to weights w; the sums so far are rescaled to the new maximum.
     __device__ static __forceinline__ void weights(const AttnCall &a, const f32x4 (&s)[SUB], State &st, int base, int p, bool whole,
-                                                   float (&w)[VKEYS]) {
+                                                   float (&w)[VKEYS], KeyRange keys) {
         const int g = lane_id() >> 4;
         float x[VKEYS];
 #pragma unroll
@@ -111,7 +111,7 @@ struct Stream {
         if (!whole) {
 #pragma unroll
             for (int r = 0; r < VKEYS; ++r)
-                if (!a.sees(p, base + (r >> 2) * 16 + g * 4 + (r & 3))) x[r] = -__builtin_inff();
+                if (!a.sees(p, base + (r >> 2) * 16 + g * 4 + (r & 3), keys)) x[r] = -__builtin_inff();
         }
         float top = x[0];
 #pragma unroll
@@ -168,8 +168,8 @@ struct Stream {
     // The tiles [x0, x1) of a row of blocks, tiles apart by STEP.
     template <int STEP>
     __device__ static __forceinline__ void run(const AttnCall &a, const u32x4 (&q)[KSTEPS], State &st, const KeyTiles<KT> &tiles, int x0, int x1,
-                                               int b, int64_t head_off, int p, int p_min, int p_max) {
-        const int last = a.last_key(p_max);
+                                               int b, int64_t head_off, int p, int p_min, int p_max, KeyRange keys = KeyRange()) {
+        const int last = a.last_key(p_max, keys);
         // A tile's key registers are free once its scores are there, its value registers once they are added: the next
         // tile's rows are asked for at these two places, so one tile's registers keep a tile's loads in flight all the time.
         // Loads come back in the order they were sent; page numbers are asked for two tiles ahead, for when their rows are
@@ -192,13 +192,13 @@ struct Stream {
             scores(t, q, s);
             const int64_t at = place(a, next, head_off, base(i + 1), last);
             load_keys(a, t, at);
-            weights(a, s, st, base(i), p, tile_whole<KT>(a, base(i), p_min, p_max), w);
+            weights(a, s, st, base(i), p, tile_whole<KT>(a, base(i), p_min, p_max, keys), w, keys);
             add_values(t, w, st);
             load_values(a, t, at);
             next = after;
         }
         scores(t, q, s);
-        weights(a, s, st, base(count - 1), p, tile_whole<KT>(a, base(count - 1), p_min, p_max), w);
+        weights(a, s, st, base(count - 1), p, tile_whole<KT>(a, base(count - 1), p_min, p_max, keys), w, keys);
         add_values(t, w, st);
     }
 

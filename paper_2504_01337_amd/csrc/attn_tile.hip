@@ -93,31 +93,56 @@ __device__ __forceinline__ float add_pair(float v, uint32_t pair) {
 // ANY_SCALE: the loop takes maxima of scores before their scale and hides keys by scores of -infinity, so the scale there is positive.
 // A negative one becomes the queries' sign, and with 0 the queries are 0 (or NaN, where the definition gives one).  A form of its own,
 // as this costs every block some 0.2 us: 32 prompts of 300 43.4 us for 42.7.
-template <int D, bool ALIGNED, bool ANY_SCALE>
+// SHARED: the rows are (sequence, head of the group) pairs of a run of sequences, one token each at its own position, and the keys those
+// that the run's sequences begin with: partial results only.
+template <int D, bool ALIGNED, bool ANY_SCALE, bool SHARED>
 __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void attn_tile_kernel(AttnCall a) {
     using T = TileShape<D>;
     constexpr int KT = T::KT, KSTEPS = D / 16, DT = D / 32, VALU = 0x2, MFMA = 0x8, DS_READ = 0x100;
     __shared__ __align__(1024) unsigned char lds[2][2][T::BYTES];  // [buffer][K, V]
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, n = lane & 31;
     int64_t id = blockIdx.x;
-    const int split = (int)(id % a.splits);
-    id /= a.splits;
+    const int splits = SHARED ? a.prefix_splits : a.splits;
+    const int split = (int)(id % splits);
+    id /= splits;
     const int kv_head = (int)(id % a.kv.kv_heads);
     id /= a.kv.kv_heads;
-    int b, rb;
-    if (!a.block_of<T::BM>((int)id, b, rb)) return;
-    const int len = a.kv.tokens(b), fresh = a.new_tokens(b), rows = min(fresh, a.max_q) * a.group;
+    int b, rb, rows, before = 0;  // before: the position of row 0's token
+    KeyRange keys;
+    if constexpr (SHARED) {
+        int run;
+        if (!a.prefix_block_of<T::BM>((int)id, run, rb, rows)) return;
+        b = a.shared_first(run), keys.to = a.shared_keys(run);
+    } else {
+        if (!a.block_of<T::BM>((int)id, b, rb)) return;
+        const int len = a.kv.tokens(b), fresh = a.new_tokens(b);
+        rows = min(fresh, a.max_q) * a.group;
+        before = len - fresh;
+    }
     const int block0 = rb * T::BM;
     if (block0 >= rows) return;
-    const int before = len - fresh;
     const int block_rows = min(rows - block0, T::BM);
-    // the block's range of positions, and this wave's
-    const int bp_min = before + block0 / a.group, bp_max = before + (block0 + block_rows - 1) / a.group, last = a.last_key(bp_max);
+    auto position = [&](int i) { return SHARED ? a.kv.tokens(b + i) - 1 : before + i; };
     const int row0 = block0 + wave * 32, left = min(rows - row0, 32);
-    const int wr0 = min(row0, rows - 1), wr1 = min(row0 + 31, rows - 1);
-    const int p_min = before + wr0 / a.group, p_max = before + wr1 / a.group;
-    const int row = min(row0 + n, rows - 1), i = row / a.group, p = before + i;
-    const int64_t token = a.first_row(b) + i;
+    const int row = min(row0 + n, rows - 1), i = row / a.group, p = position(i);
+    // the block's range of positions, and this wave's
+    int bp_min, bp_max, p_min, p_max;
+    if constexpr (SHARED) {
+        auto range = [&](int p0, int p1, int &lo, int &hi) {
+            lo = min(p0, p1), hi = max(p0, p1);
+#pragma unroll
+            for (int w = 32; w; w >>= 1) lo = min(lo, __shfl_xor(lo, w)), hi = max(hi, __shfl_xor(hi, w));
+            lo = __builtin_amdgcn_readfirstlane(lo), hi = __builtin_amdgcn_readfirstlane(hi);
+        };
+        range(p, p, p_min, p_max);
+        range(position((block0 + min(lane, block_rows - 1)) / a.group), position((block0 + min(lane + 64, block_rows - 1)) / a.group), bp_min, bp_max);
+    } else {
+        const int wr0 = min(row0, rows - 1), wr1 = min(row0 + 31, rows - 1);
+        bp_min = before + block0 / a.group, bp_max = before + (block0 + block_rows - 1) / a.group;
+        p_min = before + wr0 / a.group, p_max = before + wr1 / a.group;
+    }
+    const int last = a.last_key(bp_max, keys);
+    const int64_t token = (SHARED ? b : a.first_row(b)) + i;
     const int head = kv_head * a.group + row - i * a.group;
     const unsigned char *q_row = a.q + token * a.q_bytes + (int64_t)head * (D * 2);
     bf16x8 q[KSTEPS];
@@ -135,16 +160,17 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void attn_tile_kernel(AttnCa
     }
     const float scale = ANY_SCALE ? a.scale_size : a.scale_log2;
 
-    const KeyTiles<KT> tiles(a, bp_min, bp_max);
+    const KeyTiles<KT> tiles(a, bp_min, bp_max, keys);
     int x0, x1;
-    tiles.part(a, split, x0, x1);
-    const bool uncut = tiles.uncut(a);
+    if constexpr (SHARED) tiles.part(splits, a.prefix_tiles, split, x0, x1);
+    else tiles.part(a, split, x0, x1);
+    const bool uncut = !SHARED && tiles.uncut(a);
     const int64_t part_rows = a.T * a.heads;
     if (uncut && split > 0) return;
-    if (a.splits > 1 && (uncut || x0 == x1)) {
+    if ((SHARED || a.splits > 1) && (uncut || x0 == x1)) {
         for (int r = threadIdx.x; r < block_rows; r += 256) {
             const int rr = block0 + r, ir = rr / a.group;
-            float *ml = a.part_ml + ((int64_t)split * part_rows + (a.first_row(b) + ir) * a.heads + kv_head * a.group + rr - ir * a.group) * 2;
+            float *ml = a.part_ml + ((int64_t)split * part_rows + ((SHARED ? b : a.first_row(b)) + ir) * a.heads + kv_head * a.group + rr - ir * a.group) * 2;
             ml[0] = -__builtin_inff(), ml[1] = uncut ? PART_DONE : PART_EMPTY;
         }
         if (!uncut) return;
@@ -244,7 +270,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void attn_tile_kernel(AttnCa
         wait_copies_but<0>();
         lds_barrier();
         // (a wave that sees nothing of a tile that others of its block see goes along: every weight comes out as zero)
-        const bool whole = tile_whole<KT>(a, base, p_min, p_max);
+        const bool whole = tile_whole<KT>(a, base, p_min, p_max, keys);
         f32x16 s[2];
         bf16x8 kf[2][KSTEPS];
         u32x4 vf[2][2][DT], w[2][2];  // V and weights of 32 keys: two products of 16 keys
@@ -266,7 +292,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void attn_tile_kernel(AttnCa
             // in keys from this lane's first one on; worked out here and nowhere before (few tiles need it)
             int first = base + u * 32;
             asm volatile("" : "+s"(first));
-            const int at = first + h * 4, to = a.last_key(p) - at, from = a.window ? p - a.window - at : -1, sinks = a.window ? a.sinks - at : 0;
+            const int at = first + h * 4, to = a.last_key(p, keys) - at, from = a.window ? p - a.window - at : -1, sinks = a.window ? a.sinks - at : 0;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int c = (e >> 2) * 8 + (e & 3);
@@ -445,11 +471,12 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void attn_tile_kernel(AttnCa
         const int c = __ffsll((unsigned long long)redo) - 1;
         redo &= redo - 1;
         const int rc = row0 + c, ic = rc / a.group, hc = kv_head * a.group + rc - ic * a.group;
-        const int64_t tc = a.first_row(b) + ic;
+        const int64_t tc = (SHARED ? b : a.first_row(b)) + ic;
+        const int pc = position(ic);
         float me, le, v[D / 64];
-        exact_row<true, D, KT>(a, tiles, x0, x1, 1, b, kv_head, before + ic, a.q + tc * a.q_bytes + (int64_t)hc * (D * 2), me, le, v);
+        exact_row<true, D, KT>(a, tiles, x0, x1, 1, b, kv_head, pc, a.q + tc * a.q_bytes + (int64_t)hc * (D * 2), me, le, v, keys);
         if (uncut) {
-            const float inv = a.blind(before + ic) ? 0.0f : 1.0f / le;
+            const float inv = a.blind(pc) ? 0.0f : 1.0f / le;
             uint16_t *out = reinterpret_cast<uint16_t *>(a.out + tc * a.out_bytes + (int64_t)hc * (D * 2)) + lane * (D / 64);
 #pragma unroll
             for (int e = 0; e < D / 64; ++e) out[e] = (uint16_t)f32_to_bf16_bits(v[e] * inv);
@@ -457,19 +484,34 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void attn_tile_kernel(AttnCa
             const int64_t prow = (int64_t)split * part_rows + tc * a.heads + hc;
 #pragma unroll
             for (int e = 0; e < D / 64; ++e) a.part_o[prow * D + lane * (D / 64) + e] = v[e];
-            if (lane == 0) a.part_ml[prow * 2] = me, a.part_ml[prow * 2 + 1] = a.blind(before + ic) ? PART_EMPTY : le;
+            if (lane == 0) a.part_ml[prow * 2] = me, a.part_ml[prow * 2 + 1] = a.blind(pc) ? PART_EMPTY : le;
         }
     }
 }
 
+static bool tile_aligned(const KvView &kv) {
+    return kv.page_size % 16 == 0 && kv.page_bytes < (1ll << 32) && kv.page_size * kv.slot_bytes < (1ll << 32);
+}
+
+template <int D, bool SHARED>
+static void tile(const AttnCall &a, dim3 grid, hipStream_t st) {
+    const dim3 block(256);
+    if (!(a.scale_log2 > 0.0f)) attn_tile_kernel<D, false, true, SHARED><<<grid, block, 0, st>>>(a);
+    else if (tile_aligned(a.kv)) attn_tile_kernel<D, true, false, SHARED><<<grid, block, 0, st>>>(a);
+    else attn_tile_kernel<D, false, false, SHARED><<<grid, block, 0, st>>>(a);
+}
+
 int launch_attn_tile(const AttnCall &a, int D, hipStream_t st) {
-    const dim3 grid((unsigned)((int64_t)a.splits * a.kv.kv_heads * a.row_blocks * (a.by_rows ? 1 : a.kv.batch))), block(256);
-    const bool aligned = a.kv.page_size % 16 == 0 && a.kv.page_bytes < (1ll << 32) && a.kv.page_size * a.kv.slot_bytes < (1ll << 32);
-    if (!(a.scale_log2 > 0.0f)) D == 128 ? attn_tile_kernel<128, false, true><<<grid, block, 0, st>>>(a) : attn_tile_kernel<64, false, true><<<grid, block, 0, st>>>(a);
-    else if (D == 128) aligned ? attn_tile_kernel<128, true, false><<<grid, block, 0, st>>>(a) : attn_tile_kernel<128, false, false><<<grid, block, 0, st>>>(a);
-    else aligned ? attn_tile_kernel<64, true, false><<<grid, block, 0, st>>>(a) : attn_tile_kernel<64, false, false><<<grid, block, 0, st>>>(a);
+    const dim3 grid((unsigned)((int64_t)a.splits * a.kv.kv_heads * a.row_blocks * (a.by_rows ? 1 : a.kv.batch)));
+    D == 128 ? tile<128, false>(a, grid, st) : tile<64, false>(a, grid, st);
     const int rc = launch_status();
     return rc == C2R_OK && a.splits > 1 ? launch_attn_join(a, true, D, st) : rc;
+}
+
+int launch_attn_tile_prefix(const AttnCall &a, int D, hipStream_t st) {
+    const dim3 grid((unsigned)((int64_t)a.prefix_splits * a.kv.kv_heads * a.prefix_blocks));
+    D == 128 ? tile<128, true>(a, grid, st) : tile<64, true>(a, grid, st);
+    return launch_status();
 }
 
 }  // namespace c2r

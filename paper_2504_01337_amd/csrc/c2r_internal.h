@@ -24,6 +24,11 @@ static inline int launch_status() {
 
 static inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
+// Rows of `width` elements, `stride` apart, that the kernels touch 16 bytes at a time.
+static inline bool rows_ok(const void *p, int64_t stride, int64_t width, int size) {
+    return p && aligned(p, 16) && stride >= width && stride <= (1ll << 40) && stride * size % 16 == 0;
+}
+
 static inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 // Memory that a launch reads or writes (no bytes, or a null pointer: none).

@@ -1,0 +1,197 @@
+// The residual's sum and the root-mean-square norm of whole rows, with the rows in bf16 or fp32, in 8 bits with a scale each, or both:
+//     s = x + r (rounded as it is kept),  y = s * rsqrt(mean(s^2) + eps) * weight,  c = max |y| / 448,  y8 = y / c
+// A row is read once: its elements stay in the registers of the lanes that loaded them, 8 at a time, while the two numbers that
+// a whole row has to give (the sum of squares, then the largest |y|) go round.  Bound by memory.
+#include "c2r_internal.h"
+
+namespace c2r {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+struct NormCall {
+    const unsigned char *x, *r;  // r null: s = x
+    const float *weight;
+    unsigned char *sum, *y, *y8;  // each may be null
+    float *scale;
+    int64_t x_bytes, r_bytes, sum_bytes, y_bytes, y8_bytes;  // from one row to the next
+    int64_t T;
+    int d;
+    float eps;
+};
+
+constexpr float E4M3_MOST = 448.0f;
+constexpr float LEAST_SCALE = 1.1754943508222875e-38f;  // 2^-126: its reciprocal is finite
+
+template <bool BF16>
+__device__ __forceinline__ void load8(const unsigned char *p, float (&v)[8]) {
+    if constexpr (BF16) {
+        const u32x4 w = *reinterpret_cast<const u32x4 *>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    } else {
+        const f32x4 a = reinterpret_cast<const f32x4 *>(p)[0], b = reinterpret_cast<const f32x4 *>(p)[1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+    }
+}
+
+template <bool BF16>
+__device__ __forceinline__ void store8(unsigned char *p, const float (&v)[8]) {
+    if constexpr (BF16) {
+        *reinterpret_cast<u32x4 *>(p) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+    } else {
+        reinterpret_cast<f32x4 *>(p)[0] = f32x4{v[0], v[1], v[2], v[3]};
+        reinterpret_cast<f32x4 *>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
+    }
+}
+
+// What THREADS threads of a block have, added up (or the largest), in all of them.
+template <int THREADS, bool MAX>
+__device__ __forceinline__ float row_total(float v, float *lds) {
+    auto both = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
+#pragma unroll
+    for (int w = 32; w; w >>= 1) v = both(v, __shfl_xor(v, w));
+    if constexpr (THREADS > 64) {
+        const int wave = threadIdx.x >> 6;
+        if (lane_id() == 0) lds[wave] = v;
+        __syncthreads();
+        v = lds[0];
+#pragma unroll
+        for (int w = 1; w < THREADS / 64; ++w) v = both(v, lds[w]);
+    }
+    return v;
+}
+
+// THREADS threads to a row, PIECES pieces of 8 elements to a thread.
+template <bool BF16, int THREADS, int PIECES>
+__global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void row_norm_kernel(NormCall a) {
+    constexpr int BLOCK = THREADS > 256 ? THREADS : 256, SZ = BF16 ? 2 : 4;
+    __shared__ float sums[BLOCK / 64], tops[BLOCK / 64];
+    const int64_t t = (int64_t)blockIdx.x * (BLOCK / THREADS) + threadIdx.x / THREADS;
+    if (t >= a.T) return;  // (a whole wave, or with more threads than a wave to a row, the whole block)
+    const int lane = threadIdx.x % THREADS, pieces = a.d / 8;
+    const unsigned char *x = a.x + t * a.x_bytes, *r = a.r + t * a.r_bytes;
+    float s[PIECES][8];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int p = i * THREADS + lane;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[i][e] = 0.0f;
+        if (p < pieces) load8<BF16>(x + (int64_t)p * (8 * SZ), s[i]);
+    }
+    if (a.r) {
+        float more[PIECES][8];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int p = i * THREADS + lane;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) more[i][e] = 0.0f;
+            if (p < pieces) load8<BF16>(r + (int64_t)p * (8 * SZ), more[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                s[i][e] += more[i][e], s[i][e + 1] += more[i][e + 1];
+                if constexpr (BF16) {  // the norm is that of the sum as it is kept, whether this call writes it or not
+                    const uint32_t w = pack_bf16x2(s[i][e], s[i][e + 1]);
+                    s[i][e] = __uint_as_float(w << 16), s[i][e + 1] = __uint_as_float(w & 0xffff0000u);
+                }
+            }
+    }
+    float squares = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) squares = __builtin_fmaf(s[i][e], s[i][e], squares);
+    squares = row_total<THREADS, false>(squares, sums);
+    const float by = 1.0f / sqrtf(squares / (float)a.d + a.eps);
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int p = i * THREADS + lane;
+        if (p >= pieces) continue;
+        if (a.sum) store8<BF16>(a.sum + t * a.sum_bytes + (int64_t)p * (8 * SZ), s[i]);
+        float w[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
+        if (a.weight) load8<false>(reinterpret_cast<const unsigned char *>(a.weight + (int64_t)p * 8), w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[i][e] = s[i][e] * by * w[e], top = fmaxf(top, fabsf(s[i][e]));
+        if (a.y) store8<BF16>(a.y + t * a.y_bytes + (int64_t)p * (8 * SZ), s[i]);
+    }
+    if (!a.y8) return;
+    top = row_total<THREADS, true>(top, tops);
+    const float c = fmaxf(top / E4M3_MOST, LEAST_SCALE), inv = 1.0f / c;
+    if (lane == 0) a.scale[t] = c;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int p = i * THREADS + lane;
+        if (p >= pieces) continue;
+        u32x2 w = {0, 0};
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float *v = &s[i][4 * e];
+            const int low = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * inv, v[1] * inv, 0, false);
+            w[e] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2] * inv, v[3] * inv, low, true);
+        }
+#endif
+        *reinterpret_cast<u32x2 *>(a.y8 + t * a.y8_bytes + (int64_t)p * 8) = w;
+    }
+}
+
+template <bool BF16, int THREADS, int PIECES>
+static void norm(const NormCall &a, hipStream_t st) {
+    constexpr int BLOCK = THREADS > 256 ? THREADS : 256, ROWS = BLOCK / THREADS;
+    row_norm_kernel<BF16, THREADS, PIECES><<<dim3((unsigned)((a.T + ROWS - 1) / ROWS)), dim3(BLOCK), 0, st>>>(a);
+}
+
+template <bool BF16, int THREADS>
+static void norm_by_pieces(const NormCall &a, hipStream_t st) {
+    const int pieces = (a.d / 8 + THREADS - 1) / THREADS;
+    if (pieces <= 1) norm<BF16, THREADS, 1>(a, st);
+    else if (pieces <= 2) norm<BF16, THREADS, 2>(a, st);
+    else if (pieces <= 4) norm<BF16, THREADS, 4>(a, st);
+    else norm<BF16, THREADS, 8>(a, st);
+}
+
+template <bool BF16>
+static void norm_by_rows(const NormCall &a, hipStream_t st) {
+    if (a.d > 16384) norm<BF16, 1024, 4>(a, st);
+    else if (a.d > 4096 || (a.T < 512 && a.d > 512)) norm_by_pieces<BF16, 256>(a, st);
+    else norm_by_pieces<BF16, 64>(a, st);
+}
+
+constexpr int NORM_MOST = 32768;
+
+}  // namespace c2r
+
+using namespace c2r;
+
+extern "C" int c2r_add_rms_norm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, c2r_dtype dt, int64_t T, int d,
+                                const float *weight, float eps, void *sum, int64_t sum_stride, void *y, int64_t y_stride, void *y8,
+                                int64_t y8_stride, float *scale, void *stream) {
+    drop_stale_error();
+    if (dt != C2R_F32 && dt != C2R_BF16) return C2R_ERR_INVALID_ARG;
+    if (T < 0 || d < 1 || !(eps >= 0.0f)) return C2R_ERR_INVALID_ARG;
+    if (d % 8 != 0 || d > NORM_MOST || T >= (1ll << 30)) return C2R_ERR_UNSUPPORTED;
+    if ((sum && !residual) || !y8 != !scale || (!sum && !y && !y8)) return C2R_ERR_INVALID_ARG;
+    if (T == 0) return C2R_OK;
+    const int size = dt == C2R_BF16 ? 2 : 4;
+    if (!rows_ok(x, x_stride, d, size) || (residual && !rows_ok(residual, residual_stride, d, size))) return C2R_ERR_INVALID_ARG;
+    if ((sum && !rows_ok(sum, sum_stride, d, size)) || (y && !rows_ok(y, y_stride, d, size))) return C2R_ERR_INVALID_ARG;
+    if (y8 && (!aligned(y8, 8) || y8_stride < d || y8_stride > (1ll << 40) || y8_stride % 8 != 0 || !aligned(scale, 4))) return C2R_ERR_INVALID_ARG;
+    if (weight && !aligned(weight, 16)) return C2R_ERR_INVALID_ARG;
+    NormCall a = {};
+    a.x = static_cast<const unsigned char *>(x), a.r = static_cast<const unsigned char *>(residual);
+    a.weight = weight, a.scale = scale;
+    a.sum = static_cast<unsigned char *>(sum), a.y = static_cast<unsigned char *>(y), a.y8 = static_cast<unsigned char *>(y8);
+    a.x_bytes = x_stride * size, a.r_bytes = residual_stride * size, a.sum_bytes = sum_stride * size, a.y_bytes = y_stride * size;
+    a.y8_bytes = y8_stride;
+    a.T = T, a.d = d, a.eps = eps;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (dt == C2R_BF16) norm_by_rows<true>(a, st);
+    else norm_by_rows<false>(a, st);
+    return launch_status();
+}

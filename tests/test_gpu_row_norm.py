@@ -1,0 +1,140 @@
+"""Sum and norm of whole rows on the GPU against the definition in 64 bits (oracle/serving.py).
+
+Tolerances, derived before the first run.  u = 2^-24.  The kept sum is one 32-bit addition and one rounding: equal bits.  Its norm: a
+mean of d squares (d u at most, half of it in the root), root, division, two products: (d / 2 + 8) u |y|, and the rounding to bf16,
+2^-8 |y|.  The scale is max |y| / 448: (d / 2 + 10) u of it.  In 8 bits y / scale is off by half a step, 2^-4 of the value or 2^-10 below the
+normal numbers, and by (d + 20) u."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import serving as osv
+
+pytestmark = pytest.mark.gpu
+
+U, B8 = 2.0 ** -24, 2.0 ** -8
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def c2r():
+    from paper_2504_01337_amd import c2r as m
+    m.lib()
+    return m
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _rows(seed, T, d, dtype, pad=0, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(T, d + pad, generator=g) * scale).to(DT[dtype]).cuda()[:, :d]
+
+
+def _check(got, s, weight, eps, d, dtype):
+    """(y, y8, scale) against the norm of the kept sum s."""
+    y, y8, scale = got
+    ref = osv.rms_norm(_np(s), None if weight is None else _np(weight), eps)
+    if y is not None:
+        tol = (d / 2 + 8) * U * np.abs(ref) + (B8 * np.abs(ref) if dtype == "bf16" else 0.0) + 1e-37
+        assert (np.abs(_np(y) - ref) <= tol).all()
+    if y8 is not None:
+        c = np.maximum(np.abs(ref).max(-1) / 448.0, 2.0 ** -126)
+        assert (np.abs(_np(scale) - c) <= (d / 2 + 10) * U * c).all()
+        v = ref / c[:, None]
+        tol = np.maximum(2.0 ** -4 * np.abs(v), 2.0 ** -10) + (d + 20) * U * np.abs(v)
+        assert (np.abs(_np(y8.float()) - v) <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d", [(1, 8), (3, 8), (1, 256), (517, 256), (5, 504), (2, 520), (700, 512), (1, 2048), (600, 2048), (3, 4096), (513, 4096),
+                                 (2, 4104), (2, 8192), (9, 16384), (2, 16392), (1, 32768)])
+def test_sum_and_norm(c2r, dtype, T, d):
+    x, r, w = _rows(1, T, d, dtype, pad=24), _rows(2, T, d, dtype, pad=8, scale=3.0), _rows(3, 1, d, "f32")[0].contiguous()
+    keep = (x.clone(), r.clone())
+    y, s, y8, c = c2r.add_rms_norm(x, r, w, 1e-5, bits8=True)
+    assert torch.equal(x, keep[0]) and torch.equal(r, keep[1])
+    assert torch.equal(s, (x.float() + r.float()).to(x.dtype))
+    _check((y, y8, c), s, w, 1e-5, d, dtype)
+    # one output at a time: the same bits
+    for dense, bits8 in ((True, False), (False, True)):
+        y2, s2, y82, c2 = c2r.add_rms_norm(x, r, w, 1e-5, dense=dense, bits8=bits8)
+        assert torch.equal(s2, s) and (y2 is None) == (not dense) and (y82 is None) == (not bits8)
+        assert y2 is None or torch.equal(y2, y)
+        assert y82 is None or (torch.equal(y82.view(torch.uint8), y8.view(torch.uint8)) and torch.equal(c2, c))
+    # without the residual, without the weight: the norm of the rows as they are
+    y3, none, _, _ = c2r.add_rms_norm(x, eps=0.0)
+    assert none is None
+    _check((y3, None, None), x, None, 0.0, d, dtype)
+    y4 = c2r.add_rms_norm(s, None, w, 1e-5)[0]
+    assert torch.equal(y4, y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_outputs_in_the_place_of_inputs(c2r, dtype):
+    T, d = 70, 1160
+    x, r = _rows(4, T, d, dtype), _rows(5, T, d, dtype)
+    y, s, _, _ = c2r.add_rms_norm(x, r)
+    a, b = x.clone(), r.clone()
+    c2r.add_rms_norm(a, b, out=(a, b, None, None))            # y where x was, the sum where the residual was
+    assert torch.equal(a, y) and torch.equal(b, s)
+    a, b = x.clone(), r.clone()
+    c2r.add_rms_norm(a, b, out=(b, a, None, None))
+    assert torch.equal(b, y) and torch.equal(a, s)
+    only = torch.empty_like(x)
+    c2r.add_rms_norm(x, r, out=(None, only, None, None))      # the sum alone
+    assert torch.equal(only, s)
+
+
+def test_rows_around_the_outputs_stay(c2r):
+    T, d = 5, 264
+    x, r = _rows(6, T, d, "bf16"), _rows(7, T, d, "bf16")
+    y = torch.full((T + 2, d + 16), 7.0, dtype=torch.bfloat16, device="cuda")
+    y8 = torch.full((T + 2, d + 8), 0x55, dtype=torch.uint8, device="cuda")
+    c = torch.full((T + 2,), 7.0, device="cuda")
+    c2r.add_rms_norm(x, r, out=(y[1:-1, :d], None, y8[1:-1, :d].view(torch.float8_e4m3fn), c[1:-1]))
+    ref = c2r.add_rms_norm(x, r, bits8=True)
+    assert torch.equal(y[1:-1, :d], ref[0]) and torch.equal(y8[1:-1, :d], ref[2].view(torch.uint8)) and torch.equal(c[1:-1], ref[3])
+    assert (y[0] == 7).all() and (y[-1] == 7).all() and (y[:, d:] == 7).all()
+    assert (y8[0] == 0x55).all() and (y8[-1] == 0x55).all() and (y8[:, d:] == 0x55).all() and c[0] == 7 and c[-1] == 7
+
+
+def test_zeros_extremes_and_nan(c2r):
+    d = 2048
+    x = torch.zeros((6, d), device="cuda")
+    x[1, 5] = 1.0                        # one element: its norm is sqrt(d)
+    x[2] = 1e-30                         # squares below the normal numbers, eps decides
+    x[3, 7] = float("nan")
+    x[4, 9] = float("inf")
+    x[5] = 1e-18 * torch.arange(d, device="cuda")
+    y, _, y8, c = c2r.add_rms_norm(x, eps=1e-6, bits8=True)
+    good = [0, 1, 2, 5]
+    _check((y[good], y8[good], c[good]), x[good], None, 1e-6, d, "f32")
+    assert not y[0].any() and not y8[0].float().any() and float(c[0]) == 2.0 ** -126
+    assert torch.isnan(y[3]).all() and torch.isnan(y8[3].float()).all()
+    assert torch.isnan(y[4, 9]) and torch.isnan(y8[4, 9].float())
+    assert y8[1].float().abs().max() == 448.0
+
+
+def test_two_streams_and_a_graph(c2r):
+    x, r, w = _rows(8, 300, 2048, "bf16"), _rows(9, 300, 2048, "bf16"), _rows(10, 1, 2048, "f32")[0].contiguous()
+    ref = c2r.add_rms_norm(x, r, w, bits8=True)
+    torch.cuda.synchronize()
+    streams, outs = [torch.cuda.Stream() for _ in range(2)], []
+    for i in range(10):
+        with torch.cuda.stream(streams[i % 2]):
+            outs.append(c2r.add_rms_norm(x, r, w, bits8=True))
+    torch.cuda.synchronize()
+    for o in outs:
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(o, ref))
+    x2, g = x.clone(), torch.cuda.CUDAGraph()
+    out = tuple(torch.empty_like(t) for t in ref)
+    with torch.cuda.graph(g):
+        c2r.add_rms_norm(x2, r, w, bits8=True, out=out)
+    for k in range(3):
+        x2.copy_(x * (k + 1))
+        g.replay()
+        torch.cuda.synchronize()
+        eager = c2r.add_rms_norm(x2, r, w, bits8=True)
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(out, eager))
