@@ -14,6 +14,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int LP_THREADS = 256, LP_MOST_TOP = 64, LP_MOST_PARTS = 64, LP_CANDIDATES = 1024;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
+typedef unsigned long long Key;  // a logit and its token, see key_of
+
 struct LogitsCall {
     const unsigned char *logits;
     int64_t row_bytes, T;
@@ -23,12 +25,51 @@ struct LogitsCall {
     int V, given, n, parts;
     // of every row and part: {M, s, u, -}, and its n largest
     f32x4 *stats;
-    float *part_value;
-    int32_t *part_token;
+    Key *part_keys;
 };
 
-// One token before another: the larger logit, the lower index of equal ones.
-__device__ __forceinline__ bool before(float va, int ia, float vb, int ib) { return va > vb || (va == vb && ia < ib); }
+// A logit and its token as one number, larger for what comes first: the larger logit, the lower index of equal ones (zeros of either
+// sign are equal).  0: none.
+__device__ __forceinline__ uint32_t in_order(float v) {
+    const uint32_t b = __float_as_uint(v + 0.0f);  // (-0 + 0 = 0)
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float from_order(uint32_t b) { return __uint_as_float(b ^ ((uint32_t)((int32_t)~b >> 31) | 0x80000000u)); }
+constexpr uint32_t LOWEST = 0x007fffffu;  // of -infinity
+__device__ __forceinline__ Key key_of(float v, int token) { return (Key)in_order(v) << 32 | (uint32_t)~token; }
+__device__ __forceinline__ int token_of(Key k) { return (int)~(uint32_t)k; }
+__device__ __forceinline__ float logit_of(Key k) { return from_order((uint32_t)(k >> 32)); }
+
+// Over the 64 lanes, in every lane: the largest, the sum (in one order).
+template <bool MAX>
+__device__ __forceinline__ float wave_all(float v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    auto step = [&](auto moved) {
+        const float o = __uint_as_float((uint32_t)moved);
+        v = MAX ? fmaxf(v, o) : v + o;
+    };
+    const int none = MAX ? (int)0xff800000u : 0;
+    step(__builtin_amdgcn_update_dpp(none, (int)__float_as_uint(v), 0x111, 0xf, 0xf, false));  // row_shr:1, 2, 4, 8
+    step(__builtin_amdgcn_update_dpp(none, (int)__float_as_uint(v), 0x112, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(none, (int)__float_as_uint(v), 0x114, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(none, (int)__float_as_uint(v), 0x118, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(none, (int)__float_as_uint(v), 0x142, 0xa, 0xf, false));  // row_bcast:15 into rows 1, 3
+    step(__builtin_amdgcn_update_dpp(none, (int)__float_as_uint(v), 0x143, 0xc, 0xf, false));  // row_bcast:31 into rows 2, 3
+    v = __uint_as_float(__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
+#endif
+    return v;
+}
+
+// A lower bound of the n-th largest of 64 lanes' numbers, in their order: its upper half, bit by bit.  Every lane must be active.
+__device__ __forceinline__ uint32_t wave_nth(uint32_t mine, int n) {
+    uint32_t at = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t next = at | 1u << bit;
+        if (__popcll(__ballot(mine >= next)) >= n) at = next;
+    }
+    return at;
+}
 
 template <bool BF16>
 struct Row {
@@ -83,43 +124,74 @@ struct Sums {
     }
 };
 
-__device__ __forceinline__ float block_max(float v, float *lds) {
+// The sums of a block's lanes, against its largest logit M: {M, s, u, -} in every thread.  from: what a lane's own sums are against less the
+// given M, in powers of two.
+template <class From>
+__device__ __forceinline__ f32x4 block_sums(float top, float s, float u, const From &from, f32x4 *lds) {
+    // (nothing to move where there is no sum, or where nothing is left of it: 0 times an infinity is no number)
+    auto against = [](float d, float &s, float &u) {
+        const float f = s == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(d);
+        u = f == 0.0f ? 0.0f : __builtin_fmaf(s, d, u) * f;
+        s *= f;
+    };
+    const float wave_top = wave_all<true>(top);
+    against(from(wave_top), s, u);
+    s = wave_all<false>(s), u = wave_all<false>(u);
+    if (lane_id() == 0) lds[threadIdx.x >> 6] = f32x4{wave_top, s, u, 0.0f};
+    __syncthreads();
+    f32x4 all = {-__builtin_inff(), 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int w = 32; w; w >>= 1) v = fmaxf(v, __shfl_xor(v, w));
-    __syncthreads();
-    if (lane_id() == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+    for (int w = 0; w < 4; ++w) all[0] = fmaxf(all[0], lds[w][0]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        f32x4 v = lds[w];
+        float vs = v[1], vu = v[2];
+        against((v[0] - all[0]) * LOG2E, vs, vu);
+        all[1] += vs, all[2] += vu;
+    }
+    return all;
 }
 __device__ __forceinline__ float block_sum(float v, float *lds) {
-#pragma unroll
-    for (int w = 32; w; w >>= 1) v += __shfl_xor(v, w);
+    v = wave_all<false>(v);
     __syncthreads();
     if (lane_id() == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
     return lds[0] + lds[1] + (lds[2] + lds[3]);
 }
 
-// The candidates' n first in order, written by put(place, value, token); places that no candidate fills get token -1.
+// The candidates' n first in order, written by put(place, key); places that no candidate fills get key 0.
 template <class Put>
-__device__ __forceinline__ void put_in_order(const float *value, const int *token, int count, int n, const Put &put) {
+__device__ __forceinline__ void put_in_order(const Key *keys, int count, int n, const Put &put) {
     for (int i = threadIdx.x; i < count; i += LP_THREADS) {
-        const float v = value[i];
-        const int tok = token[i];
+        const Key k = keys[i];
         int rank = 0;
-        for (int j = 0; j < count; ++j) rank += before(value[j], token[j], v, tok);
-        if (rank < n) put(rank, v, tok);
+        for (int j = 0; j < count; ++j) rank += keys[j] > k;
+        if (rank < n) put(rank, k);
     }
-    for (int i = count + threadIdx.x; i < n; i += LP_THREADS) put(i, -__builtin_inff(), -1);
+    for (int i = count + threadIdx.x; i < n; i += LP_THREADS) put(i, 0);
 }
 
-// What the sums say of a row: lane by lane the given tokens, and the entropy.
+// A place among the candidates for every lane that has one.
+__device__ __forceinline__ int take_place(bool wants, int *count) {
+    const uint64_t here = __ballot(wants);
+    int at = 0;
+    if (wants && lane_id() == __ffsll((unsigned long long)here) - 1) at = atomicAdd(count, __popcll(here));
+    if (!wants) return 0;
+    return __builtin_amdgcn_readfirstlane(at) + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(here >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)here, 0));
+}
+
+// What the sums say of a row: the entropy, and lane by lane the given tokens (first: the lane's first one's logit).
 template <bool BF16>
-__device__ __forceinline__ void put_row(const LogitsCall &a, int64_t t, const Row<BF16> &row, float M, float s, float u, float ln_s) {
+__device__ __forceinline__ float given_logit(const LogitsCall &a, int64_t t, const Row<BF16> &row, int g) {
+    const int tok = a.tokens[t * a.given + g];
+    return (uint32_t)tok < (uint32_t)a.V ? row.element(tok) : -__builtin_inff();
+}
+template <bool BF16>
+__device__ __forceinline__ void put_row(const LogitsCall &a, int64_t t, const Row<BF16> &row, float first, float M, float s, float u, float ln_s) {
     if (threadIdx.x == 0 && a.entropy) a.entropy[t] = ln_s - u / s * LN2;
     for (int g = threadIdx.x; g < a.given; g += LP_THREADS) {
-        const int tok = a.tokens[t * a.given + g];
-        a.logprob[t * a.given + g] = (uint32_t)tok < (uint32_t)a.V ? row.element(tok) - M - ln_s : -__builtin_inff();
+        const float l = g == (int)threadIdx.x ? first : given_logit<BF16>(a, t, row, g);
+        a.logprob[t * a.given + g] = (uint32_t)a.tokens[t * a.given + g] < (uint32_t)a.V ? l - M - ln_s : -__builtin_inff();
     }
 }
 
@@ -127,15 +199,20 @@ template <bool BF16>
 __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogitsCall a) {
     using R = Row<BF16>;
     constexpr int N = R::N, AHEAD = 4;
-    __shared__ float wave_lds[4], tops[LP_THREADS], cand_value[LP_CANDIDATES], shared_limit;
-    __shared__ int list[LP_THREADS], cand_token[LP_CANDIDATES], counts[2], wave_counts[4];
+    __shared__ f32x4 wave_sums[4];
+    __shared__ float tops[LP_THREADS], wave_lds[4];
+    __shared__ Key cand[LP_CANDIDATES], wave_keys[4];
+    __shared__ int list[LP_THREADS], counts[2], wave_counts[4];
     const int64_t t = blockIdx.x / a.parts;
     const int part = (int)(blockIdx.x - t * a.parts), tid = threadIdx.x;
     const R row(a, t);
+    const bool whole = a.parts == 1;
     // this part's pieces; the first part has the elements before them, the last one those behind
     const int each = (row.pieces + a.parts - 1) / a.parts, p0 = min(part * each, row.pieces), p1 = min(p0 + each, row.pieces);
     const int head = part == 0 ? row.head : 0, tail = part == a.parts - 1 ? row.tail() : 0;
     const int extra = tid < head ? tid : tid >= 128 && tid < 128 + tail ? row.V - tail + tid - 128 : -1;
+    float first = 0.0f;
+    if (whole && tid < a.given) first = given_logit<BF16>(a, t, row, tid);
     Sums sums;
     sums.clear();
     int p = p0 + tid;
@@ -150,18 +227,27 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogitsCall a) {
             sums.add(v);
         }
     }
-    for (; p < p1; p += LP_THREADS) {
-        float v[N];
-        R::open(row.piece(p), v);
-        sums.add(v);
+    if (p < p1) {  // what is left: AHEAD - 1 pieces at most, asked for together
+        u32x4 w[AHEAD - 1];
+#pragma unroll
+        for (int i = 0; i < AHEAD - 1; ++i) w[i] = row.piece(min(p + i * LP_THREADS, p1 - 1));
+#pragma unroll
+        for (int i = 0; i < AHEAD - 1; ++i) {
+            if (p + i * LP_THREADS >= p1) break;
+            float v[N];
+            R::open(w[i], v);
+            sums.add(v);
+        }
     }
     if (extra >= 0) {
         const float v[1] = {row.element(extra)};
         sums.add(v);
     }
-    const float M = block_max(sums.top, wave_lds);
-    float d = __builtin_fmaf(-M, LOG2E, sums.ref), f = sums.s == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(d);
-    float u = block_sum(sums.s == 0.0f ? 0.0f : __builtin_fmaf(sums.s, d, sums.u) * f, wave_lds), s = block_sum(sums.s * f, wave_lds);
+    tops[tid] = sums.top;
+    if (tid < 2) counts[tid] = 0;
+    const f32x4 all = block_sums(sums.top, sums.s, sums.u, [&](float M) { return __builtin_fmaf(-M, LOG2E, sums.ref); }, wave_sums);
+    const float M = all[0];
+    float s = all[1], u = all[2];
     if (M != -__builtin_inff() ? !(s > 0.0f && s < __builtin_inff() && fabsf(u) < __builtin_inff()) : s != 0.0f) {
         // powers of two of these logits are out of range (all of them the type's lowest, say), or there is an infinity or a NaN: by the
         // definition, which gives a NaN for those
@@ -179,38 +265,31 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogitsCall a) {
         if (extra >= 0) add(row.element(extra));
         s = block_sum(s, wave_lds), u = block_sum(u, wave_lds);
     }
-    const bool whole = a.parts == 1;
     const float ln_s = logf(s);
-    if (whole) put_row<BF16>(a, t, row, M, s, u, ln_s);
+    if (whole) put_row<BF16>(a, t, row, first, M, s, u, ln_s);
     else if (tid == 0) a.stats[t * a.parts + part] = f32x4{M, s, u, 0.0f};
     if (a.n == 0) return;
 
     // ---- the n largest ----
-    const bool holds = p0 + tid < p1 || extra >= 0;
+    // a number that n lanes at least reach: of every four lanes' largest the n-th, rounded down
     float limit = M;
     if (a.n > 1) {
-        tops[tid] = sums.top;
-        __syncthreads();
-        int rank = 0;
-        for (int j = 0; j < LP_THREADS; ++j) rank += before(tops[j], j, sums.top, tid);
-        if (rank == a.n - 1) shared_limit = sums.top;
-        __syncthreads();
-        limit = shared_limit;
+        const int lane = lane_id();
+        const float four = fmaxf(fmaxf(tops[lane], tops[lane + 64]), fmaxf(tops[lane + 128], tops[lane + 192]));
+        const uint32_t at = wave_nth(in_order(four), a.n);
+        limit = at <= LOWEST ? -__builtin_inff() : from_order(at);
     }
-    if (tid == 0) counts[0] = 0;
-    __syncthreads();
-    if (holds && sums.top >= limit) list[atomicAdd(&counts[0], 1)] = tid;
+    const bool listed = (p0 + tid < p1 || extra >= 0) && sums.top >= limit;
+    const int place = take_place(listed, &counts[0]);
+    if (listed) list[place] = tid;
     __syncthreads();
     const int lanes = counts[0], rounds = p1 > p0 ? (p1 - p0 + LP_THREADS - 1) / LP_THREADS : 0;
     // candidates: the listed lanes' logits from the limit on, or above it
     auto collect = [&](bool above) {
-        __syncthreads();
-        if (tid == 0) counts[1] = 0;
-        __syncthreads();
         auto take = [&](float v, int tok) {
             if (above ? v > limit : v >= limit) {
                 const int to = atomicAdd(&counts[1], 1);
-                if (to < LP_CANDIDATES) cand_value[to] = v, cand_token[to] = tok;
+                if (to < LP_CANDIDATES) cand[to] = key_of(v, tok);
             }
         };
         const int all = lanes * rounds;
@@ -226,10 +305,19 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogitsCall a) {
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
                 if (at[i] >= p1) continue;
-                float v[N];
+                float v[N], top;
                 R::open(w[i], v);
+                top = v[0];
 #pragma unroll
-                for (int e = 0; e < N; ++e) take(v[e], row.head + at[i] * N + e);
+                for (int e = 1; e < N; ++e) top = fmaxf(top, v[e]);
+                if (top < limit) continue;
+#pragma unroll 1
+                for (int e = 0; e < N; ++e) {
+                    float x = v[0];
+#pragma unroll
+                    for (int k = 1; k < N; ++k) x = e == k ? v[k] : x;
+                    take(x, row.head + at[i] * N + e);
+                }
             }
         }
         if (extra >= 0) take(row.element(extra), extra);
@@ -239,6 +327,9 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogitsCall a) {
     int count = limit == -__builtin_inff() ? LP_CANDIDATES + 1 : collect(false);
     if (count > LP_CANDIDATES) {
         // many equal ones at the limit: what is above it, then as many of them as are wanted, in order
+        __syncthreads();
+        if (tid == 0) counts[1] = 0;
+        __syncthreads();
         count = collect(true);
         if (count <= LP_CANDIDATES) {
             int want = a.n - count;
@@ -255,7 +346,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogitsCall a) {
                 if (here)
                     for (int e = 0; e < tokens; ++e)
                         if (v[e] == limit) {
-                            if (place < want) cand_value[count + place] = limit, cand_token[count + place] = first + e;
+                            if (place < want) cand[count + place] = key_of(limit, first + e);
                             ++place;
                         }
                 const int taken = min(max(want, 0), total);
@@ -272,14 +363,13 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogitsCall a) {
             next(extra >= 0 && tid >= head, &one, 1, extra);
         } else {
             // more above it than there is room for (large logits side by side in one lane's pieces): one token after another
-            float last = __builtin_inff();
-            int last_token = -1;
+            Key last = ~0ull;
             count = 0;
             for (int k = 0; k < a.n; ++k) {
-                float best = -__builtin_inff();
-                int token = row.V;
+                Key best = 0;
                 auto look = [&](float v, int tok) {
-                    if (before(last, last_token, v, tok) && (token == row.V ? v == v : before(v, tok, best, token))) best = v, token = tok;
+                    const Key here = key_of(v, tok);
+                    if (v == v && here < last && here > best) best = here;
                 };
                 for (int q = p0 + tid; q < p1; q += LP_THREADS) {
                     float v[N];
@@ -288,74 +378,71 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogitsCall a) {
                 }
                 if (extra >= 0) look(row.element(extra), extra);
                 for (int w = 32; w; w >>= 1) {
-                    const float v = __shfl_xor(best, w);
-                    const int tok = __shfl_xor(token, w);
-                    if (before(v, tok, best, token)) best = v, token = tok;
+                    const Key o = __shfl_xor(best, w);
+                    if (o > best) best = o;
                 }
                 __syncthreads();
-                if (lane_id() == 0) wave_lds[tid >> 6] = best, wave_counts[tid >> 6] = token;
+                if (lane_id() == 0) wave_keys[tid >> 6] = best;
                 __syncthreads();
                 for (int w = 0; w < 4; ++w)
-                    if (before(wave_lds[w], wave_counts[w], best, token)) best = wave_lds[w], token = wave_counts[w];
-                if (token == row.V) break;
-                if (tid == 0) cand_value[k] = best, cand_token[k] = token;
-                last = best, last_token = token, count = k + 1;
+                    if (wave_keys[w] > best) best = wave_keys[w];
+                if (best == 0) break;
+                if (tid == 0) cand[k] = best;
+                last = best, count = k + 1;
             }
         }
         __syncthreads();
     }
     const int64_t out = (whole ? t : t * a.parts + part) * a.n;
-    put_in_order(cand_value, cand_token, count, a.n, [&](int place, float v, int tok) {
-        if (whole) a.top_token[out + place] = tok, a.top_logprob[out + place] = tok < 0 ? __builtin_nanf("") : v - M - ln_s;
-        else a.part_value[out + place] = v, a.part_token[out + place] = tok;
+    put_in_order(cand, count, a.n, [&](int place, Key k) {
+        if (whole) a.top_token[out + place] = k ? token_of(k) : -1, a.top_logprob[out + place] = k ? logit_of(k) - M - ln_s : __builtin_nanf("");
+        else a.part_keys[out + place] = k;
     });
 }
 
-// The parts of a row.
+// The parts of a row.  What it reads from memory is asked for at its start.
 template <bool BF16>
 __global__ __launch_bounds__(LP_THREADS) void logprobs_join_kernel(LogitsCall a) {
-    __shared__ float wave_lds[4], value[LP_MOST_PARTS * LP_MOST_TOP], some_value[2 * LP_MOST_TOP + LP_MOST_PARTS];
-    __shared__ int token[LP_MOST_PARTS * LP_MOST_TOP], some_token[2 * LP_MOST_TOP + LP_MOST_PARTS], count, limit_token;
-    __shared__ float limit_value;
+    constexpr int HELD = 4;
+    __shared__ f32x4 wave_sums[4];
+    __shared__ Key cand[LP_MOST_PARTS * LP_MOST_TOP];
+    __shared__ int count;
     const int64_t t = blockIdx.x;
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = lane_id(), entries = a.parts * a.n;
     const Row<BF16> row(a, t);
+    const Key *keys = a.part_keys + t * entries;
     const f32x4 mine = tid < a.parts ? a.stats[t * a.parts + tid] : f32x4{-__builtin_inff(), 0.0f, 0.0f, 0.0f};
-    const float M = block_max(mine[0], wave_lds);
-    const float d = (mine[0] - M) * LOG2E, f = mine[1] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(d);
-    const float s = block_sum(mine[1] * f, wave_lds), u = block_sum(f == 0.0f ? 0.0f : __builtin_fmaf(mine[1], d, mine[2]) * f, wave_lds);
-    const float ln_s = logf(s);
-    put_row<BF16>(a, t, row, M, s, u, ln_s);
-    if (a.n == 0) return;
-    // the n-th of the first ones of every part bounds the row's n-th from below
-    const int64_t from = t * a.parts * a.n;
-    const int firsts = (a.n + a.parts - 1) / a.parts, some = firsts * a.parts;
-    if (tid < some) {
-        const int64_t at = from + tid / firsts * a.n + tid % firsts;
-        some_value[tid] = a.part_value[at], some_token[tid] = a.part_token[at];
-    }
+    // of every part the entry up to which all parts together have n
+    const int firsts = (a.n + a.parts - 1) / a.parts;
+    const Key bound = a.n > 0 && lane < a.parts ? keys[lane * a.n + firsts - 1] : 0;
+    Key held[HELD];
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) held[i] = tid + i * LP_THREADS < entries ? keys[tid + i * LP_THREADS] : 0;
+    float first = 0.0f;
+    if (tid < a.given) first = given_logit<BF16>(a, t, row, tid);
     if (tid == 0) count = 0;
-    __syncthreads();
-    // (places without a token, -infinity and -1, come behind every token here)
-    auto key = [&](int tok) { return tok < 0 ? 0x7fffffff : tok; };
-    if (tid < some) {
-        int rank = 0;
-        for (int j = 0; j < some; ++j) rank += j != tid && (before(some_value[j], key(some_token[j]), some_value[tid], key(some_token[tid])) ||
-                                                              (some_token[j] < 0 && some_token[tid] < 0 && j < tid));
-        if (rank == a.n - 1) limit_value = some_value[tid], limit_token = key(some_token[tid]);
+    const f32x4 all = block_sums(mine[0], mine[1], mine[2], [&](float M) { return (mine[0] - M) * LOG2E; }, wave_sums);
+    const float M = all[0], s = all[1], u = all[2], ln_s = logf(s);
+    put_row<BF16>(a, t, row, first, M, s, u, ln_s);
+    if (a.n == 0) return;
+    uint32_t limit = (uint32_t)(bound >> 32);
+    if (firsts == 1) {
+        limit = wave_nth(limit, a.n);
+    } else {
+        if (lane >= a.parts) limit = ~0u;
+        for (int w = 32; w; w >>= 1) limit = min(limit, (uint32_t)__shfl_xor((int)limit, w));
     }
+    auto take = [&](Key k) {
+        const bool wants = k != 0 && (uint32_t)(k >> 32) >= limit;
+        const int to = take_place(wants, &count);
+        if (wants) cand[to] = k;
+    };
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) take(held[i]);
+    for (int i = HELD * LP_THREADS + tid; i < entries; i += LP_THREADS) take(keys[i]);
     __syncthreads();
-    for (int i = tid; i < a.parts * a.n; i += LP_THREADS) {
-        const float v = a.part_value[from + i];
-        const int tok = a.part_token[from + i];
-        if (tok >= 0 && !before(limit_value, limit_token, v, tok)) {
-            const int to = atomicAdd(&count, 1);
-            value[to] = v, token[to] = tok;
-        }
-    }
-    __syncthreads();
-    put_in_order(value, token, count, a.n, [&](int place, float v, int tok) {
-        a.top_token[t * a.n + place] = tok, a.top_logprob[t * a.n + place] = tok < 0 ? __builtin_nanf("") : v - M - ln_s;
+    put_in_order(cand, count, a.n, [&](int place, Key k) {
+        a.top_token[t * a.n + place] = k ? token_of(k) : -1, a.top_logprob[t * a.n + place] = k ? logit_of(k) - M - ln_s : __builtin_nanf("");
     });
 }
 
@@ -398,8 +485,7 @@ extern "C" int c2r_token_logprobs(const void *logits, c2r_dtype dt, int64_t stri
     if (a.parts > 1) {
         if (!ws || !aligned(ws, 256) || ws_bytes < (size_t)T * a.parts * (16 + 8 * (size_t)n_top)) return C2R_ERR_WORKSPACE;
         a.stats = static_cast<f32x4 *>(ws);
-        a.part_value = reinterpret_cast<float *>(a.stats + T * a.parts);
-        a.part_token = reinterpret_cast<int32_t *>(a.part_value + T * a.parts * n_top);
+        a.part_keys = reinterpret_cast<Key *>(a.stats + T * a.parts);
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
     const dim3 grid((unsigned)(T * a.parts)), rows((unsigned)T), block(LP_THREADS);
