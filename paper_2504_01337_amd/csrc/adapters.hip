@@ -14,7 +14,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int AD_MOST_ADAPTERS = 1024, AD_MOST_RANK = 128, AD_STEP = 64;
+constexpr int AD_MOST_ADAPTERS = 1024, AD_MOST_RANK = 128;
 
 // What x holds: the weights' type, or e4m3 with a scale for every row beside bf16 weights.
 enum { AD_F32 = 0, AD_BF16 = 1, AD_E4M3 = 2 };
@@ -31,6 +31,7 @@ struct AdapterCall {
     const float *x_scale, *scale;
     int64_t x_bytes, y_bytes, out_bytes;
     int T, E, r, d_in, d_out, tile_rows, ranks16, parts, max_tiles;
+    bool in_blocks;     // the first product's blocks work the order out
     bool copy_rest;     // rows without an adapter are copied
     AdapterTile *tiles;
     int *slots;         // the row in every slot, -1: none
@@ -107,41 +108,157 @@ __global__ __launch_bounds__(1024) void adapter_order_kernel(AdapterCall a) {
     }
 }
 
+// Every block of the first product works its tile out itself where that is less work than a launch of one block ahead of it: 131 rows 17 -> 15 us
+// of a call.  A row's place among those of its adapter is that of its number.  here[]: the rows in places
+// in_tile .. + slots of the tile.  lds: 1024 + 1 + 8 words.
+constexpr int AD_FEW_ROWS = 256;
+__device__ __forceinline__ AdapterTile few_rows_tile(const AdapterCall &a, int at, int in_tile, int slots, int *here, int *lds) {
+    int *const count = lds, *const upto = lds + AD_MOST_ADAPTERS + 1, *const found = upto + 4;
+    const int tid = threadIdx.x, wave = tid >> 6;
+    const int e = tid < a.T ? a.adapter[tid] : 0, mine = tid >= a.T ? -1 : (uint32_t)e < (uint32_t)a.E ? e : a.E;
+    for (int i = tid; i <= a.E; i += 256) count[i] = 0;
+    if (tid < slots) here[tid] = -1;
+    if (tid == 0) found[0] = -1;
+    __syncthreads();
+    if (mine >= 0) atomicAdd(&count[mine], 1);
+    __syncthreads();
+    // four adapters to a thread, and the rows without one behind them
+    int tiles = 0;
+    auto tiles_of = [&](int i) { return (count[i] + a.tile_rows - 1) / a.tile_rows; };
+    for (int i = tid * 4; i < min(tid * 4 + 4, a.E); ++i) tiles += tiles_of(i);
+    const int sum = wave_inclusive_scan(tiles);
+    if (lane_id() == 63) upto[wave] = sum;
+    __syncthreads();
+    int first = sum - tiles, all = 0;
+    for (int w = 0; w < 4; ++w) first += w < wave ? upto[w] : 0, all += upto[w];
+    if (at >= first && at < first + tiles) {
+        int i = tid * 4;
+        for (; at >= first + tiles_of(i); ++i) first += tiles_of(i);
+        found[0] = i, found[1] = at - first;
+    } else if (tid == 0 && a.copy_rest && at >= all && at < all + tiles_of(a.E)) {
+        found[0] = a.E, found[1] = at - all;
+    }
+    __syncthreads();
+    const int group = found[0];
+    if (group < 0) return AdapterTile{-2, 0};
+    const uint64_t same = __ballot(mine == group);
+    if (lane_id() == 0) upto[wave] = __popcll(same);
+    __syncthreads();
+    int rank = (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0));
+    for (int w = 0; w < wave; ++w) rank += upto[w];
+    rank -= found[1] * a.tile_rows + in_tile;
+    if (mine == group && rank >= 0 && rank < slots) here[rank] = tid;
+    const AdapterTile tile = {group < a.E ? group : -1, min(count[group] - found[1] * a.tile_rows, a.tile_rows)};
+    __syncthreads();
+    return tile;
+}
+
+// The same for up to eight times as many rows, of up to 255 adapters: a wave has a quarter of the rows, and counts of its own.  (8192 rows that
+// way took 66 us of a call where the block ahead takes 59.)
+constexpr int AD_SOME_ROWS = 2048, AD_SOME_ADAPTERS = 255;
+__device__ __forceinline__ AdapterTile some_rows_tile(const AdapterCall &a, int at, int in_tile, int slots, int *here, int *lds) {
+    constexpr int EACH = AD_SOME_ROWS / 256;  // rows of a thread
+    int *const count = lds, *const upto = lds + 4 * (AD_SOME_ADAPTERS + 1), *const found = upto + 4;
+    const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6), groups = a.E + 1;
+    const int r0 = wave * (EACH * 64) + lane;
+    int g[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) g[i] = r0 + i * 64 < a.T ? a.adapter[r0 + i * 64] : 0;
+    for (int i = tid; i < 4 * groups; i += 256) count[i] = 0;
+    if (tid < slots) here[tid] = -1;
+    if (tid == 0) found[0] = -1;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        g[i] = r0 + i * 64 >= a.T ? -1 : (uint32_t)g[i] < (uint32_t)a.E ? g[i] : a.E;
+        const int first = __builtin_amdgcn_readfirstlane(g[i]);
+        if (__all(g[i] == first || g[i] < 0)) {  // (mostly rows of one request)
+            const int n = __popcll(__ballot(g[i] >= 0));
+            if (lane == 0 && n) atomicAdd(&count[wave * groups + first], n);
+        } else if (g[i] >= 0) {
+            atomicAdd(&count[wave * groups + g[i]], 1);
+        }
+    }
+    __syncthreads();
+    auto rows_of = [&](int g) { return count[g] + count[groups + g] + (count[2 * groups + g] + count[3 * groups + g]); };
+    const int tiles = tid < a.E ? (rows_of(tid) + a.tile_rows - 1) / a.tile_rows : 0, sum = wave_inclusive_scan(tiles);
+    if (lane == 63) upto[wave] = sum;
+    __syncthreads();
+    int first = sum - tiles, all = 0;
+    for (int w = 0; w < 4; ++w) first += w < wave ? upto[w] : 0, all += upto[w];
+    if (at >= first && at < first + tiles) found[0] = tid, found[1] = at - first;
+    else if (tid == 255 && a.copy_rest && at >= all && at < all + (rows_of(a.E) + a.tile_rows - 1) / a.tile_rows) found[0] = a.E, found[1] = at - all;
+    __syncthreads();
+    const int group = found[0];
+    if (group < 0) return AdapterTile{-2, 0};
+    const int from = found[1] * a.tile_rows + in_tile;
+    int rank = 0;
+    for (int w = 0; w < wave; ++w) rank += count[w * groups + group];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const uint64_t same = __ballot(g[i] == group);
+        const int mine = rank - from + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0));
+        if (g[i] == group && mine >= 0 && mine < slots) here[mine] = r0 + i * 64;
+        rank += __popcll(same);
+    }
+    const AdapterTile tile = {group < a.E ? group : -1, min(rows_of(group) - found[1] * a.tile_rows, a.tile_rows)};
+    __syncthreads();
+    return tile;
+}
+static bool rows_in_blocks(int64_t T, int E) { return T <= AD_FEW_ROWS || (T <= AD_SOME_ROWS && E <= AD_SOME_ADAPTERS); }
+
 // ---- h = A x ----
 
-// Sixteen elements of a row from `at` on, of which `left` (a multiple of 8, or none) are in it: as they lie there, and opened to bf16 or fp32.
+// 16 rows x 256 bytes of the weights' type, and the 16 rows x as many elements of x: loads in which 16 (8) neighbouring lanes are in one row, which
+// costs the memory pipe a quarter of what a lane for a row does (an address at a time; 8192 rows 14 us), then through LDS to where the matrix
+// instructions want them.  Lane l loads row 4 i + l / 16 (e4m3: 8 i + l / 8), 16-byte piece l % 16 (l % 8); lane (g, n) gets pieces 4 j + g of row n.
+// A wave's own LDS, whose accesses keep their order: nobody waits.  Piece p of row r stands at p ^ r, so that neither side meets on a bank.
 template <int X>
-struct Sixteen {
-    static constexpr int WORDS = X == AD_F32 ? 4 : X == AD_BF16 ? 2 : 1;
-    u32x4 w[WORDS];
-    __device__ __forceinline__ void load(const unsigned char *row, int at, int left) {
+struct Strip {
+    static constexpr int PER_ROW = X == AD_E4M3 ? 8 : 16, LOADS = PER_ROW / 4, ROWS = 64 / PER_ROW, PIECE = X == AD_F32 ? 4 : X == AD_BF16 ? 8 : 16;
+    u32x4 w[LOADS];
+    // row(r): where row r begins; elements from `at` on, of which `left` (a multiple of 8, or none) are in the row
+    template <class Rows>
+    __device__ __forceinline__ void load(const Rows &row, int at, int left) {
+        const int piece = lane_id() % PER_ROW * PIECE;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const bool in = left > half * 8;
-            if constexpr (X == AD_F32) {
-                const u32x4 *p = reinterpret_cast<const u32x4 *>(row + (int64_t)(at + half * 8) * 4);
-                w[half * 2] = in ? p[0] : u32x4{0, 0, 0, 0};
-                w[half * 2 + 1] = in ? p[1] : u32x4{0, 0, 0, 0};
-            } else if constexpr (X == AD_BF16) {
-                w[half] = in ? *reinterpret_cast<const u32x4 *>(row + (int64_t)(at + half * 8) * 2) : u32x4{0, 0, 0, 0};
+        for (int i = 0; i < LOADS; ++i) {
+            const unsigned char *from = row(i) + (int64_t)(at + piece) * 16 / PIECE;
+            w[i] = u32x4{0, 0, 0, 0};
+            if constexpr (X == AD_E4M3) {  // (rows of whole 8 bytes)
+                typedef u32x4 half_aligned __attribute__((aligned(8)));
+                if (left > piece + 8) {
+                    w[i] = *reinterpret_cast<const half_aligned *>(from);
+                } else if (left > piece) {
+                    const u32x2 lo = *reinterpret_cast<const u32x2 *>(from);
+                    w[i][0] = lo[0], w[i][1] = lo[1];
+                }
             } else {
-                const u32x2 v = in ? *reinterpret_cast<const u32x2 *>(row + at + half * 8) : u32x2{0, 0};
-                w[0][half * 2] = v[0], w[0][half * 2 + 1] = v[1];
+                if (left > piece) w[i] = *reinterpret_cast<const u32x4 *>(from);
             }
         }
     }
-    __device__ __forceinline__ void open(u32x4 (&to)[X == AD_F32 ? 4 : 2]) const {
-        if constexpr (X == AD_E4M3) {  // (every e4m3 number is a bf16 one)
+    __device__ __forceinline__ void hand_on(unsigned char *lds, u32x4 (&to)[4]) const {
+        const int lane = lane_id(), g = lane >> 4, n = lane & 15;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int r = i * ROWS + lane / PER_ROW;
+            *reinterpret_cast<u32x4 *>(lds + (r * PER_ROW + (lane % PER_ROW ^ r % PER_ROW)) * 16) = w[i];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (X == AD_E4M3) {  // 8 bytes; every e4m3 number is a bf16 one
+                const u32x2 v = *reinterpret_cast<const u32x2 *>(lds + (n * PER_ROW + ((j * 2 + (g >> 1)) ^ n % PER_ROW)) * 16 + (g & 1) * 8);
 #if defined(__HIP_DEVICE_COMPILE__)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w[0][i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w[0][i], true);
-                to[i >> 1][i % 2 * 2] = pack_bf16x2(lo[0], lo[1]), to[i >> 1][i % 2 * 2 + 1] = pack_bf16x2(hi[0], hi[1]);
-            }
+                for (int i = 0; i < 2; ++i) {
+                    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(v[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(v[i], true);
+                    to[j][2 * i] = pack_bf16x2(lo[0], lo[1]), to[j][2 * i + 1] = pack_bf16x2(hi[0], hi[1]);
+                }
 #endif
-        } else {
-#pragma unroll
-            for (int i = 0; i < WORDS; ++i) to[i] = w[i];
+            } else {
+                to[j] = *reinterpret_cast<const u32x4 *>(lds + (n * PER_ROW + ((j * 4 + g) ^ n)) * 16);
+            }
         }
     }
 };
@@ -159,59 +276,81 @@ __device__ __forceinline__ f32x4 multiply(const u32x4 &a, const u32x4 &b, f32x4 
     return c;
 }
 
-// Blocks: parts of d_in fastest, then 16 RG ranks, then 16 MG rows of a tile.  A wave's step is 64 elements of d_in, lane (g, n) has 16 of them of
-// rank n and of row n.
+// Blocks: parts of d_in fastest, then 16 RG ranks, then 16 MG rows of a tile.  A wave's step is 256 bytes of every rank's row (128 elements of d_in,
+// 64 in fp32), and its products leave lane (g, n) with ranks 4 g .. of row n.
 template <int X, int MG, int RG>
 __global__ __launch_bounds__(256) void adapter_down_kernel(AdapterCall a) {
     constexpr bool BF16 = X != AD_F32;
-    constexpr int W = BF16 ? AD_BF16 : AD_F32, WS = BF16 ? 2 : 4;
-    __shared__ f32x4 sums[4][MG * RG][64];
+    constexpr int W = BF16 ? AD_BF16 : AD_F32, WS = BF16 ? 2 : 4, STEP = 256 / WS;
+    __shared__ __align__(16) unsigned char strips[4][4096];
+    __shared__ f32x4 sums[MG * RG == 1 ? 5 : 4][MG * RG][64];  // (also few_rows_tile's)
+    static_assert(sizeof(sums) >= (AD_MOST_ADAPTERS + 1 + 8) * 4, "room for few_rows_tile");
     const int chunks = (a.ranks16 + RG - 1) / RG, part = blockIdx.x % a.parts, id = blockIdx.x / a.parts, chunk = id % chunks, rows_at = id / chunks;
     const int slot0 = rows_at * (MG * 16), in_tile = slot0 % a.tile_rows;
-    const AdapterTile tile = a.tiles[slot0 / a.tile_rows];
-    const int lane = lane_id(), wave = threadIdx.x >> 6, g = lane >> 4, n = lane & 15;
-    int row[MG];
+    const int lane = lane_id(), wave = threadIdx.x >> 6;
+    __shared__ int here[MG * 16];  // the rows of these slots
+    AdapterTile tile;
+    if (a.in_blocks) {
+        int *const lds = reinterpret_cast<int *>(sums);
+        tile = a.T <= AD_FEW_ROWS ? few_rows_tile(a, slot0 / a.tile_rows, in_tile, MG * 16, here, lds)
+                                  : some_rows_tile(a, slot0 / a.tile_rows, in_tile, MG * 16, here, lds);
+        if (part == 0 && chunk == 0) {  // for the second product
+            if (threadIdx.x < MG * 16) a.slots[slot0 + threadIdx.x] = here[threadIdx.x];
+            if (threadIdx.x == 0 && in_tile == 0) a.tiles[slot0 / a.tile_rows] = tile;
+        }
+    } else {
+        tile = a.tiles[slot0 / a.tile_rows];
+        if (threadIdx.x < MG * 16) here[threadIdx.x] = a.slots[slot0 + threadIdx.x];
+        __syncthreads();
+    }
+    const unsigned char *x_row[MG][Strip<X>::LOADS], *a_row[RG][Strip<W>::LOADS];
 #pragma unroll
-    for (int m = 0; m < MG; ++m) row[m] = a.slots[slot0 + m * 16 + n];
+    for (int m = 0; m < MG; ++m)
+#pragma unroll
+        for (int i = 0; i < Strip<X>::LOADS; ++i)  // (an empty slot goes along with row 0)
+            x_row[m][i] = a.x + (int64_t)max(here[m * 16 + i * Strip<X>::ROWS + lane / Strip<X>::PER_ROW], 0) * a.x_bytes;
     const int left = tile.rows - in_tile;
     if (tile.adapter < 0 || left <= 0) return;
-    const unsigned char *x_row[MG], *a_row[RG];
-#pragma unroll
-    for (int m = 0; m < MG; ++m) x_row[m] = a.x + (int64_t)max(row[m], 0) * a.x_bytes;  // (an empty slot goes along with row 0)
 #pragma unroll
     for (int q = 0; q < RG; ++q)
-        a_row[q] = a.A + ((int64_t)tile.adapter * a.r + min((chunk * RG + q) * 16 + n, a.r - 1)) * ((int64_t)a.d_in * WS);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            a_row[q][i] = a.A + ((int64_t)tile.adapter * a.r + min((chunk * RG + q) * 16 + i * 4 + lane / 16, a.r - 1)) * ((int64_t)a.d_in * WS);
     f32x4 acc[MG][RG];
 #pragma unroll
     for (int m = 0; m < MG; ++m)
 #pragma unroll
         for (int q = 0; q < RG; ++q) acc[m][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const int steps = (a.d_in + AD_STEP - 1) / AD_STEP, each = (steps + a.parts - 1) / a.parts;
+    const int steps = (a.d_in + STEP - 1) / STEP, each = (steps + a.parts - 1) / a.parts;
     const int s1 = min((part + 1) * each, steps);
     // (DEPTH steps are asked for together)
-    constexpr int DEPTH = MG * RG == 1 ? 8 : MG * RG <= 4 ? 4 : 2;
+    constexpr int DEPTH = MG * RG == 1 ? 4 : MG * RG <= 4 ? 2 : 1;
     for (int s = part * each + wave; s < s1; s += 4 * DEPTH) {
-        Sixteen<X> xs[DEPTH][MG];
-        Sixteen<W> as[DEPTH][RG];
+        Strip<X> xs[DEPTH][MG];
+        Strip<W> as[DEPTH][RG];
 #pragma unroll
         for (int i = 0; i < DEPTH; ++i) {
-            const int k = (s + 4 * i) * AD_STEP + g * 16, in = s + 4 * i < s1 ? a.d_in - k : 0;
+            const int k = (s + 4 * i) * STEP, in = s + 4 * i < s1 ? a.d_in - k : 0;
 #pragma unroll
-            for (int q = 0; q < RG; ++q) as[i][q].load(a_row[q], k, in);
+            for (int q = 0; q < RG; ++q) as[i][q].load([&](int l) { return a_row[q][l]; }, k, in);
 #pragma unroll
-            for (int m = 0; m < MG; ++m) xs[i][m].load(x_row[m], k, in);
+            for (int m = 0; m < MG; ++m) xs[i][m].load([&](int l) { return x_row[m][l]; }, k, in);
         }
 #pragma unroll
-        for (int i = 0; i < DEPTH; ++i)
+        for (int i = 0; i < DEPTH; ++i) {
+            u32x4 av[RG][4];
+#pragma unroll
+            for (int q = 0; q < RG; ++q) as[i][q].hand_on(strips[wave], av[q]);
 #pragma unroll
             for (int m = 0; m < MG; ++m) {
-                u32x4 x[BF16 ? 2 : 4];
-                xs[i][m].open(x);
+                u32x4 xv[4];
+                xs[i][m].hand_on(strips[wave], xv);
 #pragma unroll
                 for (int q = 0; q < RG; ++q)
 #pragma unroll
-                    for (int w = 0; w < (BF16 ? 2 : 4); ++w) acc[m][q] = multiply<BF16>(as[i][q].w[w], x[w], acc[m][q]);
+                    for (int j = 0; j < 4; ++j) acc[m][q] = multiply<BF16>(av[q][j], xv[j], acc[m][q]);
             }
+        }
     }
 #pragma unroll
     for (int m = 0; m < MG; ++m)
@@ -224,7 +363,7 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(AdapterCall a) {
         if (at >= left || rank >= a.ranks16 * 16) continue;
         f32x4 v = sums[0][mq][l] + sums[1][mq][l] + (sums[2][mq][l] + sums[3][mq][l]);
         float by = a.scale ? a.scale[tile.adapter] : 1.0f;
-        if (X == AD_E4M3) by *= a.x_scale[a.slots[slot0 + at]];
+        if (X == AD_E4M3) by *= a.x_scale[here[at]];
         v *= by;
         if (rank >= a.r) v = f32x4{0.0f, 0.0f, 0.0f, 0.0f};  // (r is a multiple of 8)
         *reinterpret_cast<f32x4 *>(a.h + ((int64_t)part * a.max_tiles * a.tile_rows + slot0 + at) * (a.ranks16 * 16) + rank) = v;
@@ -456,7 +595,8 @@ extern "C" int c2r_adapters(const void *x, int64_t x_stride, const float *x_scal
     a.slots = reinterpret_cast<int *>(w + p.tile_bytes);
     a.h = reinterpret_cast<float *>(w + p.tile_bytes + p.slot_bytes);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    adapter_order_kernel<<<dim3(1), dim3(1024), 0, st>>>(a);
+    a.in_blocks = rows_in_blocks(T, n_adapters);
+    if (!a.in_blocks) adapter_order_kernel<<<dim3(1), dim3(1024), 0, st>>>(a);
     if (dt == C2R_F32) adapter_products<AD_F32>(a, p, st);
     else if (x_scale) adapter_products<AD_E4M3>(a, p, st);
     else adapter_products<AD_BF16>(a, p, st);

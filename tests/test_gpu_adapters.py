@@ -96,6 +96,20 @@ def test_many_adapters_of_one_row(c2r):
     c.check(c.run(c2r))
 
 
+@pytest.mark.parametrize("T,n", [(257, 255), (257, 256), (1000, 3), (2048, 7), (2049, 7), (9000, 2), (17000, 5), (5000, 1000)])
+@pytest.mark.parametrize("each", [1, 150])
+def test_many_rows(c2r, T, n, each):
+    """Either way in which rows find their places: all rows once, requests of a row or of many, some rows without."""
+    rng = np.random.default_rng(T + n)
+    ids = np.repeat(rng.integers(-1, n, -(-T // each)), each)[:T]
+    c = Case("bf16", T, 64, 32, 8, n, ids, seed=T)
+    c.check(c.run(c2r))
+    keep = c.y.clone()
+    out = c.run(c2r)
+    c.y = keep.clone()
+    assert torch.equal(c.run(c2r, out=c.y), out)
+
+
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
 def test_a_row_alone_and_among_others(c2r, kind):
     """What a row gets is within the tolerance whatever rows stand beside it, NaN and infinities in others and in other adapters included."""
