@@ -313,22 +313,21 @@ extern "C" int c2r_attention_decode_shared(const void *q, int64_t q_stride, int 
     const bool tiled = bf16 && cache->batch * a.group > ATTN_PREFIX_ROWS * n_shared;
     const int64_t per_block = tiled ? ATTN_TILE_ROWS : 16, KT = tiled ? 64 : bf16 ? 32 : 16;
     const int64_t rows = cache->batch * a.group / per_block + n_shared, prefix_tiles = ceil_div(longest(cache, max_shared_len), KT);
-    int64_t parts = attn_parts(rows * cache->kv_heads, prefix_tiles, tiled ? ATTN_TILE_BLOCKS : ATTN_DECODE_BLOCKS, tiled ? ATTN_TILE_TILES : ATTN_DECODE_TILES);
+    int64_t parts = attn_parts(rows * cache->kv_heads, prefix_tiles, tiled ? ATTN_PREFIX_BLOCKS : ATTN_DECODE_BLOCKS, tiled ? ATTN_TILE_TILES : ATTN_DECODE_TILES);
+    // (no more blocks than CUs: one too many takes as long as as many again)
+    if (tiled && parts > 1 && parts * rows * cache->kv_heads > ATTN_PREFIX_BLOCKS) --parts;
     a.prefix_tiles = (int)ceil_div(prefix_tiles, parts);
     a.prefix_splits = (int)ceil_div(prefix_tiles, a.prefix_tiles);
     a.prefix_blocks = (int)rows;
     // what lies behind them
     const int64_t blocks = cache->batch * cache->kv_heads * ceil_div(a.group, 16);
     const int64_t tiles = attn_max_tiles(a, bf16 ? 32 : 16, 1, longest(cache, max_own_len));
-    attn_split(a, tiles, decode_parts(blocks, tiles));
+    // many sequences with few keys each: a wave for each, of 8 tiles at most
+    a.own_by_wave = blocks >= ATTN_WAVE_SETS && tiles <= ATTN_WAVE_MOST;
+    attn_split(a, tiles, a.own_by_wave ? ceil_div(tiles, ATTN_WAVE_TILES) : decode_parts(blocks, tiles));
     if (rows * cache->kv_heads * a.prefix_splits + blocks * a.splits >= ATTN_MOST_BLOCKS) return C2R_ERR_UNSUPPORTED;
     a.splits += a.prefix_splits;
     rc = place_parts(a, D, ws, ws_bytes);
     if (rc != C2R_OK) return rc;
-    if (tiled) {
-        rc = launch_attn_tile_prefix(a, D, static_cast<hipStream_t>(stream));
-        if (rc != C2R_OK) return rc;
-        a.prefix_blocks = 0;
-    }
-    return launch_attn_shared(a, bf16, D, static_cast<hipStream_t>(stream));
+    return launch_attn_shared(a, bf16, tiled, D, static_cast<hipStream_t>(stream));
 }

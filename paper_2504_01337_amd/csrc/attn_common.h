@@ -83,6 +83,7 @@ struct AttnCall {
     // prefix_tiles tiles, the others from the sequences' own keys.  prefix_blocks: rows of blocks that the prefixes have.
     const int32_t *shared_start, *shared_len;
     int shared, prefix_splits, prefix_tiles, prefix_blocks;
+    bool own_by_wave;  // a sequence's own keys are one wave's, for the heads of a key head, and not a block's
     float *part_o, *part_ml;  // [splits][T * heads][D] sums, [splits][T * heads][2] maximum and denominator (or PART_..)
 
     __device__ __forceinline__ int first_row(int b) const { return q_start ? (int)clamp_row(q_start[b]) : b; }
@@ -111,20 +112,41 @@ struct AttnCall {
     }
     __device__ __forceinline__ int shared_first(int i) const { return (int)clamp_row(shared_start[i]); }
     __device__ __forceinline__ int shared_keys(int i) const { return min(max(shared_len[i], 0), kv.capacity); }
-    // The run that sequence b is in, -1: none.
-    __device__ __forceinline__ int run_of(int b) const {
-        const int i = count_first(shared, [&](int r) { return shared_first(r) <= b; }) - 1;
-        return i >= 0 && b < shared_first(i + 1) ? i : -1;
+    // A run: its sequences first .. end - 1, and its keys.  The last run that begins at or below x by begin(run, its first sequence); -1: none.
+    struct Run {
+        int i, first, end, keys;
+    };
+    template <class F>
+    __device__ __forceinline__ Run run_at(int x, const F &begin) const {
+        Run run;
+        if (shared <= C2R_WAVE) {  // one run to a lane: all that is to be known comes with one trip to memory
+            const int r = min(lane_id(), shared - 1), first = shared_first(r), end = shared_first(r + 1), keys = shared_keys(r);
+            run.i = __popcll(__ballot(lane_id() < shared && begin(r, first) <= x)) - 1;
+            const int at = max(run.i, 0);
+            run.first = __shfl(first, at), run.end = __shfl(end, at), run.keys = __shfl(keys, at);
+        } else {
+            run.i = count_first(shared, [&](int r) { return begin(r, shared_first(r)) <= x; }) - 1;
+            const int at = max(run.i, 0);
+            run.first = shared_first(at), run.end = shared_first(at + 1), run.keys = shared_keys(at);
+        }
+        run.first = __builtin_amdgcn_readfirstlane(run.first), run.end = __builtin_amdgcn_readfirstlane(run.end);
+        run.keys = __builtin_amdgcn_readfirstlane(run.keys);
+        return run;
     }
-    // Block x of a key head's and part's: run i and block rb of its (sequence, head of the group) rows, counted as in block_of.
+    // The keys that sequence b has before its own ones.
+    __device__ __forceinline__ int prefix_of(int b) const {
+        const Run run = run_at(b, [](int, int first) { return first; });
+        return run.i >= 0 && b < run.end ? run.keys : 0;
+    }
+    // Block x of a key head's and part's: a run and block rb of its (sequence, head of the group) rows, counted as in block_of.
     template <int BM>
-    __device__ __forceinline__ bool prefix_block_of(int x, int &i, int &rb, int &rows) const {
-        auto begin = [&](int r) { return (int)((int64_t)shared_first(r) * group / BM) + r; };
-        i = count_first(shared, [&](int r) { return begin(r) <= x; }) - 1;
-        if (i < 0) return false;
-        rows = (shared_first(i + 1) - shared_first(i)) * group;
-        rb = x - begin(i);
-        return rb * BM < rows && shared_keys(i) > 0;
+    __device__ __forceinline__ bool prefix_block_of(int x, Run &run, int &rb, int &rows) const {
+        auto begin = [&](int r, int first) { return (int)((int64_t)first * group / BM) + r; };
+        run = run_at(x, begin);
+        if (run.i < 0) return false;
+        rows = (run.end - run.first) * group;
+        rb = x - begin(run.i, run.first);
+        return rb * BM < rows && run.keys > 0;
     }
     // The last key that is cached of those up to position p, and of those the last one of keys[.., to).
     __device__ __forceinline__ int last_key(int p) const { return min(p, kv.capacity - 1); }
@@ -251,9 +273,7 @@ int launch_attn_join(const AttnCall &a, bool bf16, int D, hipStream_t st);
 // attn_decode.hip: one new token per sequence.
 int launch_attn_decode(const AttnCall &a, bool bf16, int D, hipStream_t st);
 // attn_shared.hip: one new token per sequence behind prefixes that runs of sequences share.
-int launch_attn_shared(const AttnCall &a, bool bf16, int D, hipStream_t st);
-// attn_tile.hip: the parts of a shared prefix, bf16.
-int launch_attn_tile_prefix(const AttnCall &a, int D, hipStream_t st);
+int launch_attn_shared(const AttnCall &a, bool bf16, bool tiled, int D, hipStream_t st);
 // attn_rows.hip: prompts in full precision.
 int launch_attn_rows_f32(const AttnCall &a, int D, hipStream_t st);
 // attn_tile.hip: prompts in bf16, key tiles through LDS.
@@ -274,8 +294,11 @@ constexpr int ATTN_BY_ROWS = 2;
 // Blocks of a join from which on keys are not cut: nearly all of them would find nothing to do.
 constexpr int64_t ATTN_JOIN_BLOCKS = 1 << 17;
 
-// Rows of a shared prefix, per key head, from which on its keys go through LDS.
-constexpr int ATTN_PREFIX_ROWS = 32;
+// Rows of a shared prefix, per key head, from which on its keys go through LDS; the blocks of 128 rows that its parts make at most: one to a CU, beside
+// the sequences' own keys.  131 sequences of 32 / 8 heads behind 8000 keys with up to 500 each, in 3, 4, 5, 6, 7 parts: 80, 68, 60, 61, 69 us.
+constexpr int ATTN_PREFIX_ROWS = 32, ATTN_PREFIX_BLOCKS = 256;
+// Own keys by waves (attn_shared.hip): parts of 8 tiles, where no sequence has more than two and there are enough of them.
+constexpr int ATTN_WAVE_TILES = 8, ATTN_WAVE_MOST = 16, ATTN_WAVE_SETS = 768;
 constexpr int64_t ATTN_MOST_RUNS = 1 << 20;
 
 // A grid's threads are counted in 32 bits.
