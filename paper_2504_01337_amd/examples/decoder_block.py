@@ -1,13 +1,17 @@
 """A decoder block around the MoE layer, and a stack of them that takes prompts and then a token at a time.
 
-    x = x + attention(norm(x)) . W_o        qk_norm_rope_append, then attention_prefill or attention_decode
+    x = x + attention(norm(x)) . W_o        add_rms_norm, qk_norm_rope_append, then attention_prefill or attention_decode
     x = x + moe(norm(x))                    C2RLayer
+
+Requests may have low-rank adapters of their own beside the two projections (adapters), may begin with one prompt that is kept and read once
+for all of them (Decoder.share, attention_decode_shared), and their answers are scored against a vocabulary (Decoder.logprobs, token_logprobs).
 
     python -m paper_2504_01337_amd.examples.decoder_block                     # small, fp32
     python -m paper_2504_01337_amd.examples.decoder_block --workload C3       # 2048 wide, 60 experts + shared, bf16
+    python -m paper_2504_01337_amd.examples.decoder_block --adapters 3 --common 400 --vocab 1000
 
 Weights are random (workloads.py); hidden states stand in for embedded tokens, and the last block's output is the next token's
-input.  The projections and the norms of whole rows are torch's."""
+input.  The projections are torch's."""
 import argparse
 import time
 
@@ -43,23 +47,46 @@ class DecoderBlock:
         idx, _, _ = c2r.route(on(wl.hidden(w, max(w.T_profile // 16, w.T)), self.dtype), self.Wg, self.bias, w.K)
         self.collab, _ = c2r.collaborators(c2r.build_coactivation(idx, w.E), w.Tc)
         self.moe = {}
+        self.adapters = None
+
+    def add_adapters(self, n, rank, scale=1.0, seed=0):
+        """n adapters beside both projections, for requests to choose from: (A, B) of each, and their scales."""
+        dev = self.w_qkv.device
+        gen = torch.Generator(device=dev).manual_seed(seed)
+        normal = lambda *s: torch.randn(s, generator=gen, device=dev).mul_(s[2] ** -0.5).to(self.dtype)
+        pair = lambda w: (normal(n, rank, w.shape[1]), normal(n, w.shape[0], rank))
+        self.adapters = (pair(self.w_qkv), pair(self.w_o), torch.full((n,), scale, device=dev))
+
+    def _project(self, x, which, adapter):
+        """Rows through the query, key and value projection (0) or the output's (1), with the requests' adapters."""
+        y = torch.nn.functional.linear(x, (self.w_qkv, self.w_o)[which])
+        if adapter is not None and self.adapters is not None:
+            A, B = self.adapters[which]
+            c2r.adapters(x, adapter, A, B, y, self.adapters[2], out=y)
+        return y
 
     def cache(self, n_pages, page_size, batch, max_pages):
         return c2r.PagedKVCache.empty(n_pages, page_size, self.kv_heads, self.head_dim, batch, max_pages, self.dtype)
 
-    def forward(self, x, cache, q_start=None, max_new=1, max_kv_len=0):
+    def forward(self, x, cache, q_start=None, max_new=1, max_kv_len=0, adapter=None, shared=None):
         """x[T, d]: the new rows of all sequences, which cache.kv_len already counts.  q_start[batch + 1]: where each sequence's
-        begin; None: one of each."""
+        begin; None: one of each.  adapter: int32[T], each row's.  shared: (shared_start, shared_len, the longest) of runs of sequences
+        that begin with the same keys, for single new rows."""
         T, H, Hkv, D = len(x), self.heads, self.kv_heads, self.head_dim
-        qkv = torch.nn.functional.linear(rms_norm(x), self.w_qkv).view(T, H + 2 * Hkv, D)
+        rows = c2r.add_rms_norm(x)[0]
+        qkv = self._project(rows, 0, adapter).view(T, H + 2 * Hkv, D)
         q = c2r.qk_norm_rope_append(qkv[:, :H], qkv[:, H:H + Hkv], qkv[:, H + Hkv:], cache, self.inv_freq, q_start, None,
                                     self.q_weight, self.k_weight)
-        if q_start is None:
+        if q_start is None and shared is not None:
+            start, keys, longest = shared
+            o = c2r.attention_decode_shared(q, cache, start, keys, window=self.window, sinks=self.sinks, max_shared_len=longest,
+                                            max_own_len=max(max_kv_len - longest, 1))
+        elif q_start is None:
             o = c2r.attention_decode(q, cache, window=self.window, sinks=self.sinks, max_kv_len=max_kv_len)
         else:
             o = c2r.attention_prefill(q, cache, q_start, max_new, window=self.window, sinks=self.sinks, max_kv_len=max_kv_len)
-        x = x + torch.nn.functional.linear(o.view(T, H * D), self.w_o)
-        return x + self._layer(T).forward(rms_norm(x))
+        rows, x, _, _ = c2r.add_rms_norm(self._project(o.view(T, H * D), 1, adapter), x)
+        return x + self._layer(T).forward(rows)
 
     def _layer(self, T):
         layer = self.moe.pop(T, None)
@@ -75,8 +102,12 @@ class DecoderBlock:
 class Decoder:
     """Blocks and their caches.  All blocks of a batch share the page table and the lengths: a page is the same slots in each."""
 
-    def __init__(self, blocks, batch, max_len, page_size=64):
-        self.blocks, self.max_len = blocks, max_len
+    def __init__(self, blocks, batch, max_len, page_size=64, adapter=None, vocab=0):
+        """adapter: int32[batch] on the device, each sequence's (see DecoderBlock.add_adapters; -1: none).  vocab: tokens that logprobs
+        scores against (random rows)."""
+        self.blocks, self.max_len, self.adapter, self.shared = blocks, max_len, adapter, None
+        d = blocks[0].w.d
+        self.head = torch.randn((vocab, d), generator=torch.Generator().manual_seed(vocab)).mul_(d ** -0.5).to(blocks[0].w_qkv) if vocab else None
         per = -(-max_len // page_size)
         first = blocks[0].cache(batch * per, page_size, batch, per)
         first.page_table.copy_(torch.randperm(batch * per, dtype=torch.int32).view(batch, per))
@@ -97,8 +128,38 @@ class Decoder:
             raise ValueError(f"sequence {lengths.index(max(lengths))} would have {max(lengths)} rows, the caches hold {self.max_len}")
         self.lengths = lengths
 
+    def share(self, x):
+        """A common beginning x[n, d] of all sequences, while they are empty: its rows go through the blocks once, as the first sequence's (with no
+        adapter), whole pages of its keys become everyone's, and steps read them once for all.  Returns the last block's rows."""
+        if any(self.lengths):
+            raise ValueError("a common beginning comes first")
+        n, batch = len(x), len(self.lengths)
+        adapter, self.adapter = self.adapter, None
+        y = self.prompt(x, [n] + [0] * (batch - 1))
+        self.adapter = adapter
+        table, size = self.caches[0].page_table, self.caches[0].k.shape[2]
+        whole, part = n // size, n % size
+        table[1:, :whole] = table[0, :whole]
+        if part:
+            here, there = table[0, whole].long(), table[1:, whole].long()
+            for c in self.caches:
+                c.k[there, :, :part], c.v[there, :, :part] = c.k[here, :, :part], c.v[here, :, :part]
+        self.kv_len[1:] = n
+        self.lengths = [n] * batch
+        i32 = dict(dtype=torch.int32, device=x.device)
+        self.shared = (torch.tensor([0, batch], **i32), torch.tensor([n], **i32), n)
+        return y
+
+    def logprobs(self, x, tokens=None, n_top=0):
+        """token_logprobs of the last block's rows x[T, d]."""
+        return c2r.token_logprobs(torch.nn.functional.linear(c2r.add_rms_norm(x)[0], self.head), tokens, n_top)
+
     def reset(self):
         """Empty sequences."""
+        if self.shared is not None:             # (pages that were everyone's: each has its own again)
+            table = self.caches[0].page_table
+            table.copy_(torch.randperm(table.numel(), dtype=torch.int32).view(table.shape))
+            self.shared = None
         self.kv_len.zero_()
         self.lengths = [0] * len(self.lengths)
 
@@ -110,8 +171,9 @@ class Decoder:
         q_start[1:] = new.cumsum(0)
         q_start, new = q_start.cuda(), new.cuda()
         self.kv_len += new
+        adapter = None if self.adapter is None else torch.repeat_interleave(self.adapter, new, output_size=len(x))
         for block, cache in zip(self.blocks, self.caches):
-            x = block.forward(x, cache, q_start, max(lengths), self.max_len)
+            x = block.forward(x, cache, q_start, max(lengths), self.max_len, adapter)
         return x
 
     def step(self, x):
@@ -119,7 +181,7 @@ class Decoder:
         self._grow([1] * len(self.lengths))
         self.kv_len += 1
         for block, cache in zip(self.blocks, self.caches):
-            x = block.forward(x, cache, max_kv_len=self.max_len)
+            x = block.forward(x, cache, max_kv_len=self.max_len, adapter=self.adapter, shared=self.shared)
         return x
 
 
@@ -131,11 +193,20 @@ def main():
     ap.add_argument("--sinks", type=int, default=0)
     ap.add_argument("--prompts", type=int, nargs="+", default=[500, 37, 1, 260])
     ap.add_argument("--steps", type=int, default=32)
+    ap.add_argument("--adapters", type=int, default=0, help="low-rank adapters that the sequences have in turn")
+    ap.add_argument("--common", type=int, default=0, help="rows that all sequences begin with")
+    ap.add_argument("--vocab", type=int, default=0, help="score the last rows against so many tokens")
     a = ap.parse_args()
     w = wl.WORKLOADS[a.workload]
     head_dim = 64 if w.d < 1024 else 128
-    block = lambda i: DecoderBlock(w, w.d // head_dim, w.d // head_dim, head_dim, a.window, a.sinks, seed=i)
-    dec = Decoder([block(i) for i in range(a.blocks)], len(a.prompts), max(a.prompts) + a.steps + 1)
+    def block(i):
+        b = DecoderBlock(w, w.d // head_dim, w.d // head_dim, head_dim, a.window, a.sinks, seed=i)
+        if a.adapters:
+            b.add_adapters(a.adapters, 16, 0.1, seed=i)
+        return b
+    adapter = (torch.arange(len(a.prompts), dtype=torch.int32) % a.adapters).cuda() if a.adapters else None
+    dec = Decoder([block(i) for i in range(a.blocks)], len(a.prompts), a.common + max(a.prompts) + a.steps + 1, adapter=adapter, vocab=a.vocab)
+    common = torch.randn(a.common, w.d, device="cuda").to(dec.blocks[0].dtype)
     x = torch.randn(sum(a.prompts), w.d, device="cuda").to(dec.blocks[0].dtype)
 
     def timed(f, *args):
@@ -146,6 +217,8 @@ def main():
         return y, time.perf_counter() - t
     dec.prompt(x, a.prompts)                    # (first calls load the kernels)
     dec.reset()
+    if a.common:
+        dec.share(common)
     y, t = timed(dec.prompt, x, a.prompts)
     print(f"{w.name}: {len(x)} rows of {len(a.prompts)} prompts through {a.blocks} blocks: {t * 1e3:.2f} ms")
     last = rms_norm(y[torch.tensor(a.prompts).cumsum(0).cuda() - 1])
@@ -158,6 +231,10 @@ def main():
     last, t = timed(steps, last)
     assert torch.isfinite(last).all()
     print(f"{a.steps} steps of {len(a.prompts)} sequences: {t / a.steps * 1e3:.3f} ms a step")
+    if a.vocab:
+        _, entropy, top, logprob = dec.logprobs(last, n_top=min(3, a.vocab))
+        print("likeliest tokens", top.tolist(), "log probabilities", [[round(v, 3) for v in r] for r in logprob.tolist()],
+              "entropy", [round(v, 3) for v in entropy.tolist()])
 
 
 if __name__ == "__main__":
