@@ -553,12 +553,22 @@ def attention_decode_shared(q, cache, shared_start, shared_len, scale=None, wind
     B, H, D = q.shape
     dt, n = cache.dtype, shared_len.shape[0]
     assert B == cache.batch and D == cache.head_dim
-    out = torch.empty((B, H, D), dtype=dt, device=q.device) if out is None else out
+    L, q_at = lib(), _rows(q, B, H, D, dt)
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out_at = (out.data_ptr(), H * D)
+    else:
+        out_at = _rows(out, B, H, D, dt)
     if ws is None:
-        ws = torch.empty(lib().c2r_workspace_bytes(STAGE_ATTENTION_SHARED, B, D, H, cache.kv_heads, 0, 0), dtype=torch.uint8, device=q.device)
-    _check("c2r_attention_decode_shared", lib().c2r_attention_decode_shared(
-        *_rows(q, B, H, D, dt), H, cache.args, _vec(shared_start, torch.int32, n + 1), _vec(shared_len, torch.int32, n), n, max_shared_len,
-        max_own_len, D ** -0.5 if scale is None else scale, window, sinks, *_rows(out, B, H, D, dt), ws.data_ptr(), ws.numel(), _raw_stream()))
+        ws_bytes = L.c2r_workspace_bytes(STAGE_ATTENTION_SHARED, B, D, H, cache.kv_heads, 0, 0)
+        ws = q.new_empty((ws_bytes,), dtype=torch.uint8)
+    else:
+        ws_bytes = ws.numel()
+    rc = L.c2r_attention_decode_shared(
+        *q_at, H, cache.args, _vec(shared_start, torch.int32, n + 1), _vec(shared_len, torch.int32, n), n, max_shared_len, max_own_len,
+        D ** -0.5 if scale is None else scale, window, sinks, *out_at, ws.data_ptr(), ws_bytes, _raw_stream())
+    if rc != OK:
+        raise C2RError("c2r_attention_decode_shared", rc)
     return out
 
 
@@ -566,8 +576,9 @@ def _matrix(t: Optional[torch.Tensor], T, d, dtype):
     """(address, elements from one row to the next) of rows [T, d], or of none."""
     if t is None:
         return None, 0
-    assert t.shape == (T, d) and t.dtype is dtype and t.is_cuda and (t.stride(1) == 1 or d == 1), "device-resident rows [T, d] of one type"
-    return t.data_ptr(), t.stride(0) if T > 1 else -(-d // 8) * 8
+    s = t.stride()
+    assert t.shape == (T, d) and t.dtype is dtype and t.is_cuda and (s[1] == 1 or d == 1), "device-resident rows [T, d] of one type"
+    return t.data_ptr(), s[0] if T > 1 else -(-d // 8) * 8
 
 
 def add_rms_norm(x, residual=None, weight=None, eps=1e-6, dense=True, bits8=False, out=None):
@@ -576,15 +587,21 @@ def add_rms_norm(x, residual=None, weight=None, eps=1e-6, dense=True, bits8=Fals
     sum may be inputs.  Returns these four."""
     T, d = x.shape
     dt = x.dtype
+    x_at, r_at, w_at = _matrix(x, T, d, dt), _matrix(residual, T, d, dt), _vec(weight, torch.float32, d)
     if out is None:
-        out = (torch.empty((T, d), dtype=dt, device=x.device) if dense else None,
-               None if residual is None else torch.empty((T, d), dtype=dt, device=x.device),
-               torch.empty((T, d), dtype=torch.float8_e4m3fn, device=x.device) if bits8 else None,
-               torch.empty((T,), dtype=torch.float32, device=x.device) if bits8 else None)
-    y, total, y8, scale = out
-    _check("c2r_add_rms_norm", lib().c2r_add_rms_norm(
-        *_matrix(x, T, d, dt), *_matrix(residual, T, d, dt), _dt(x), T, d, _vec(weight, torch.float32, d), eps, *_matrix(total, T, d, dt),
-        *_matrix(y, T, d, dt), *_matrix(y8, T, d, torch.float8_e4m3fn), _vec(scale, torch.float32, T), _raw_stream()))
+        # (what is made here needs no look at its strides; the host's time is more than the kernel's for a few rows)
+        new = lambda: torch.empty_like(x, memory_format=torch.contiguous_format)
+        y, total, y8, scale = out = (new() if dense else None, None if residual is None else new(),
+                                     x.new_empty((T, d), dtype=torch.float8_e4m3fn) if bits8 else None,
+                                     x.new_empty((T,), dtype=torch.float32) if bits8 else None)
+        at = (0 if total is None else total.data_ptr(), d, 0 if y is None else y.data_ptr(), d, 0 if y8 is None else y8.data_ptr(), d,
+              0 if scale is None else scale.data_ptr())
+    else:
+        y, total, y8, scale = out
+        at = (*_matrix(total, T, d, dt), *_matrix(y, T, d, dt), *_matrix(y8, T, d, torch.float8_e4m3fn), _vec(scale, torch.float32, T))
+    rc = lib().c2r_add_rms_norm(*x_at, *r_at, _dt(x), T, d, w_at, eps, *at, _raw_stream())
+    if rc != OK:
+        raise C2RError("c2r_add_rms_norm", rc)
     return out
 
 
@@ -596,13 +613,22 @@ def adapters(x, adapter, A, B, y, scale=None, x_scale=None, ws=None, out=None):
     n, r, _ = A.shape
     d_out, dt = B.shape[1], A.dtype
     assert A.shape[2] == d_in and B.shape == (n, d_out, r) and B.dtype is dt
-    out = torch.empty((T, d_out), dtype=dt, device=x.device) if out is None else out
+    L, y_at = lib(), _matrix(y, T, d_out, dt)
+    if out is None:
+        out = torch.empty_like(y, memory_format=torch.contiguous_format)
+        out_at = (out.data_ptr(), d_out)
+    else:
+        out_at = y_at if out is y else _matrix(out, T, d_out, dt)
     if ws is None:
-        ws = torch.empty(max(256, lib().c2r_workspace_bytes(STAGE_ADAPTERS, T, d_in, n, r, 0, 0)), dtype=torch.uint8, device=x.device)
-    _check("c2r_adapters", lib().c2r_adapters(
+        ws_bytes = L.c2r_workspace_bytes(STAGE_ADAPTERS, T, d_in, n, r, 0, 0)
+        ws = x.new_empty((ws_bytes,), dtype=torch.uint8)
+    else:
+        ws_bytes = ws.numel()
+    rc = L.c2r_adapters(
         *_matrix(x, T, d_in, dt if x_scale is None else torch.float8_e4m3fn), _vec(x_scale, torch.float32, T), _dt(A), T, d_in, d_out,
-        _vec(adapter, torch.int32, T), n, r, _ptr(A), _ptr(B), _vec(scale, torch.float32, n), *_matrix(y, T, d_out, dt),
-        *_matrix(out, T, d_out, dt), ws.data_ptr(), ws.numel(), _raw_stream()))
+        _vec(adapter, torch.int32, T), n, r, _addr(A), _addr(B), _vec(scale, torch.float32, n), *y_at, *out_at, ws.data_ptr(), ws_bytes, _raw_stream())
+    if rc != OK:
+        raise C2RError("c2r_adapters", rc)
     return out
 
 
@@ -610,23 +636,36 @@ def token_logprobs(logits, tokens=None, n_top=0, entropy=True, ws=None, out=None
     """From logits[T, V] the log probabilities of tokens[T, n] (int32; or [T], or None), the entropy and the n_top likeliest tokens with theirs,
     equal logits by the lower index.  Returns (logprob, entropy, top_token, top_logprob), None what is not asked for."""
     T, V = logits.shape
-    dev = logits.device
-    assert logits.is_cuda and (V == 1 or logits.stride(1) == 1)
-    given = 0
+    strides = logits.stride()
+    assert logits.is_cuda and (V == 1 or strides[1] == 1)
+    L, given = lib(), 0
     if tokens is not None:
         assert tokens.dtype is torch.int32 and tokens.is_cuda and tokens.is_contiguous() and tokens.shape[0] == T
         given = tokens.numel() // T if T else 0
     if out is None:
-        f32 = dict(dtype=torch.float32, device=dev)
-        out = (torch.empty(tokens.shape, **f32) if given else None, torch.empty((T,), **f32) if entropy else None,
-               torch.empty((T, n_top), dtype=torch.int32, device=dev) if n_top else None, torch.empty((T, n_top), **f32) if n_top else None)
-    lp, ent, top, top_lp = out
-    if ws is None:
-        need = lib().c2r_workspace_bytes(STAGE_LOGPROBS, T, V, 1, n_top, 0, 0)
-        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    _check("c2r_token_logprobs", lib().c2r_token_logprobs(
-        logits.data_ptr(), _dt(logits), logits.stride(0) if T > 1 else V, T, V, _addr(tokens), given, n_top, _addr(lp), _addr(ent), _addr(top),
-        _addr(top_lp), 0 if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _raw_stream()))
+        f32 = torch.float32
+        lp, ent, top, top_lp = out = (logits.new_empty(tokens.shape, dtype=f32) if given else None, logits.new_empty((T,), dtype=f32) if entropy else None,
+                                      logits.new_empty((T, n_top), dtype=torch.int32) if n_top else None,
+                                      logits.new_empty((T, n_top), dtype=f32) if n_top else None)
+        at = [0 if t is None else t.data_ptr() for t in out]
+    else:
+        lp, ent, top, top_lp = out
+        for t, shape, dtype in ((lp, tokens.shape if given else None, torch.float32), (ent, (T,), torch.float32), (top, (T, n_top), torch.int32),
+                                (top_lp, (T, n_top), torch.float32)):
+            assert t is None or (t.shape == shape and t.dtype is dtype)
+        at = [_addr(t) for t in out]
+    ws_at = ws_bytes = 0
+    if ws is not None:
+        ws_at, ws_bytes = ws.data_ptr(), ws.numel()
+    else:
+        ws_bytes = L.c2r_workspace_bytes(STAGE_LOGPROBS, T, V, 1, n_top, 0, 0)
+        if ws_bytes:
+            ws = logits.new_empty((ws_bytes,), dtype=torch.uint8)
+            ws_at = ws.data_ptr()
+    rc = L.c2r_token_logprobs(logits.data_ptr(), _dt(logits), strides[0] if T > 1 else V, T, V, _addr(tokens), given, n_top, *at, ws_at, ws_bytes,
+                              _raw_stream())
+    if rc != OK:
+        raise C2RError("c2r_token_logprobs", rc)
     return out
 
 
