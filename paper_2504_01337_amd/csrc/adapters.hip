@@ -376,7 +376,7 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(AdapterCall a) {
 // are in different rows takes an address at a time (64 cycles; 8192 x 6144 in bf16 51 us), so they go through LDS, 16 rows at a time, and y and
 // out are touched in whole stretches of a row, 512 bytes by half a wave (45 us), and pass by the caches (38).  STEPS: products that r takes (32 ranks each in bf16, 16 in fp32);
 // B's rows for all of them, y and h are asked for together.
-template <bool BF16, int MG, int STEPS>
+template <bool BF16, int MG, int STEPS, bool STREAMED>
 __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterCall a) {
     constexpr int SZ = BF16 ? 2 : 4, KS = BF16 ? 32 : 16, E16 = 16 / SZ, PITCH = STEPS * KS + E16;  // (rows four banks apart)
     constexpr int SLOTS = MG * 16, QUADS = STEPS * KS / 4, H = (SLOTS * QUADS + 255) / 256;
@@ -410,8 +410,16 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterCall a) {
     for (int m = 0; m < MG; ++m)
 #pragma unroll
         for (int p = 0; p < PIECES; ++p)
-            if (in(m, p)) y[m][p] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(a.y + (int64_t)row[m][p] * a.y_bytes + (int64_t)mine * SZ));
-    auto put = [&](int m, int p, const u32x4 &w) { __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>(a.out + (int64_t)row[m][p] * a.out_bytes + (int64_t)mine * SZ)); };
+            if (in(m, p)) {
+                const u32x4 *from = reinterpret_cast<const u32x4 *>(a.y + (int64_t)row[m][p] * a.y_bytes + (int64_t)mine * SZ);
+                if constexpr (STREAMED) y[m][p] = __builtin_nontemporal_load(from);
+                else y[m][p] = *from;
+            }
+    auto put = [&](int m, int p, const u32x4 &w) {
+        u32x4 *to = reinterpret_cast<u32x4 *>(a.out + (int64_t)row[m][p] * a.out_bytes + (int64_t)mine * SZ);
+        if constexpr (STREAMED) __builtin_nontemporal_store(w, to);
+        else *to = w;
+    };
     if (tile.adapter < 0) {
 #pragma unroll
         for (int m = 0; m < MG; ++m)
@@ -542,22 +550,22 @@ static void adapter_down(const AdapterCall &a, const AdapterPlan &p, hipStream_t
     else adapter_down_kernel<X, MG, 4><<<grid, block, 0, st>>>(a);
 }
 
+template <bool BF16, int MG, bool STREAMED>
+static void adapter_up(const AdapterCall &a, const AdapterPlan &p, hipStream_t st) {
+    constexpr int ONE = BF16 ? 1 : 2;  // products of 32 ranks
+    const dim3 grid((unsigned)(p.tiles * ((a.d_out + 255) / 256))), block(256);
+    if (p.ranks16 <= 2) adapter_up_kernel<BF16, MG, ONE, STREAMED><<<grid, block, 0, st>>>(a);
+    else if (p.ranks16 <= 4) adapter_up_kernel<BF16, MG, 2 * ONE, STREAMED><<<grid, block, 0, st>>>(a);
+    else adapter_up_kernel<BF16, MG, 4 * ONE, STREAMED><<<grid, block, 0, st>>>(a);
+}
+
 template <int X>
 static void adapter_products(const AdapterCall &a, const AdapterPlan &p, hipStream_t st) {
     if (p.down_rows == 64) adapter_down<X, 4>(a, p, st);
     else adapter_down<X, 1>(a, p, st);
-    const dim3 grid((unsigned)(p.tiles * ((a.d_out + 255) / 256))), block(256);
-    constexpr bool BF16 = X != AD_F32;
-    constexpr int ONE = BF16 ? 1 : 2;  // products of 32 ranks
-    if (p.tile_rows == 64) {
-        if (p.ranks16 <= 2) adapter_up_kernel<BF16, 4, ONE><<<grid, block, 0, st>>>(a);
-        else if (p.ranks16 <= 4) adapter_up_kernel<BF16, 4, 2 * ONE><<<grid, block, 0, st>>>(a);
-        else adapter_up_kernel<BF16, 4, 4 * ONE><<<grid, block, 0, st>>>(a);
-    } else {
-        if (p.ranks16 <= 2) adapter_up_kernel<BF16, 1, ONE><<<grid, block, 0, st>>>(a);
-        else if (p.ranks16 <= 4) adapter_up_kernel<BF16, 1, 2 * ONE><<<grid, block, 0, st>>>(a);
-        else adapter_up_kernel<BF16, 1, 4 * ONE><<<grid, block, 0, st>>>(a);
-    }
+    const bool streamed = (int64_t)a.T * a.d_out * (X == AD_F32 ? 4 : 2) >= STREAMED_BYTES;
+    if (p.tile_rows == 64) streamed ? adapter_up<X != AD_F32, 4, true>(a, p, st) : adapter_up<X != AD_F32, 4, false>(a, p, st);
+    else streamed ? adapter_up<X != AD_F32, 1, true>(a, p, st) : adapter_up<X != AD_F32, 1, false>(a, p, st);
 }
 
 }  // namespace c2r

@@ -29,6 +29,9 @@ static inline bool rows_ok(const void *p, int64_t stride, int64_t width, int siz
     return p && aligned(p, 16) && stride >= width && stride <= (1ll << 40) && stride * size % 16 == 0;
 }
 
+// Results (or operands) of one call from this size on are more than the L2s hold for whoever comes next: they are streamed past them.
+constexpr int64_t STREAMED_BYTES = 32ll << 20;
+
 static inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 // Memory that a launch reads or writes (no bytes, or a null pointer: none).

@@ -71,7 +71,8 @@ __device__ __forceinline__ uint32_t wave_nth(uint32_t mine, int n) {
     return at;
 }
 
-template <bool BF16>
+// STREAMED: each logit is wanted once and there are many: they pass by the caches (4096 rows of 128200 in bf16: 173 us, and 194 the other way).
+template <bool BF16, bool STREAMED = false>
 struct Row {
     static constexpr int SZ = BF16 ? 2 : 4, N = 16 / SZ;  // elements of a 16-byte piece
     const unsigned char *at;
@@ -85,7 +86,11 @@ struct Row {
         if constexpr (BF16) return bf16_bits_to_f32(reinterpret_cast<const uint16_t *>(at)[i]);
         return reinterpret_cast<const float *>(at)[i];
     }
-    __device__ u32x4 piece(int p) const { return *reinterpret_cast<const u32x4 *>(at + ((int64_t)head + (int64_t)p * N) * SZ); }
+    __device__ u32x4 piece(int p) const {
+        const u32x4 *from = reinterpret_cast<const u32x4 *>(at + ((int64_t)head + (int64_t)p * N) * SZ);
+        if constexpr (STREAMED) return __builtin_nontemporal_load(from);
+        return *from;
+    }
     __device__ static void open(const u32x4 &w, float (&v)[N]) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -181,24 +186,24 @@ __device__ __forceinline__ int take_place(bool wants, int *count) {
 }
 
 // What the sums say of a row: the entropy, and lane by lane the given tokens (first: the lane's first one's logit).
-template <bool BF16>
-__device__ __forceinline__ float given_logit(const LogitsCall &a, int64_t t, const Row<BF16> &row, int g) {
+template <class R>
+__device__ __forceinline__ float given_logit(const LogitsCall &a, int64_t t, const R &row, int g) {
     const int tok = a.tokens[t * a.given + g];
     return (uint32_t)tok < (uint32_t)a.V ? row.element(tok) : -__builtin_inff();
 }
-template <bool BF16>
-__device__ __forceinline__ void put_row(const LogitsCall &a, int64_t t, const Row<BF16> &row, float first, float M, float s, float u, float ln_s) {
+template <class R>
+__device__ __forceinline__ void put_row(const LogitsCall &a, int64_t t, const R &row, float first, float M, float s, float u, float ln_s) {
     if (threadIdx.x == 0 && a.entropy) a.entropy[t] = ln_s - u / s * LN2;
     for (int g = threadIdx.x; g < a.given; g += LP_THREADS) {
-        const float l = g == (int)threadIdx.x ? first : given_logit<BF16>(a, t, row, g);
+        const float l = g == (int)threadIdx.x ? first : given_logit(a, t, row, g);
         a.logprob[t * a.given + g] = (uint32_t)a.tokens[t * a.given + g] < (uint32_t)a.V ? l - M - ln_s : -__builtin_inff();
     }
 }
 
-template <bool BF16>
+template <bool BF16, bool STREAMED>
 __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogitsCall a) {
-    using R = Row<BF16>;
-    constexpr int N = R::N, AHEAD = 4;
+    using R = Row<BF16, STREAMED>;
+    constexpr int N = R::N, AHEAD = STREAMED ? 8 : 4;
     __shared__ f32x4 wave_sums[4];
     __shared__ float tops[LP_THREADS], wave_lds[4];
     __shared__ Key cand[LP_CANDIDATES], wave_keys[4];
@@ -212,7 +217,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogitsCall a) {
     const int head = part == 0 ? row.head : 0, tail = part == a.parts - 1 ? row.tail() : 0;
     const int extra = tid < head ? tid : tid >= 128 && tid < 128 + tail ? row.V - tail + tid - 128 : -1;
     float first = 0.0f;
-    if (whole && tid < a.given) first = given_logit<BF16>(a, t, row, tid);
+    if (whole && tid < a.given) first = given_logit(a, t, row, tid);
     Sums sums;
     sums.clear();
     int p = p0 + tid;
@@ -266,7 +271,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogitsCall a) {
         s = block_sum(s, wave_lds), u = block_sum(u, wave_lds);
     }
     const float ln_s = logf(s);
-    if (whole) put_row<BF16>(a, t, row, first, M, s, u, ln_s);
+    if (whole) put_row(a, t, row, first, M, s, u, ln_s);
     else if (tid == 0) a.stats[t * a.parts + part] = f32x4{M, s, u, 0.0f};
     if (a.n == 0) return;
 
@@ -419,11 +424,11 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_join_kernel(LogitsCall a)
 #pragma unroll
     for (int i = 0; i < HELD; ++i) held[i] = tid + i * LP_THREADS < entries ? keys[tid + i * LP_THREADS] : 0;
     float first = 0.0f;
-    if (tid < a.given) first = given_logit<BF16>(a, t, row, tid);
+    if (tid < a.given) first = given_logit(a, t, row, tid);
     if (tid == 0) count = 0;
     const f32x4 all = block_sums(mine[0], mine[1], mine[2], [&](float M) { return (mine[0] - M) * LOG2E; }, wave_sums);
     const float M = all[0], s = all[1], u = all[2], ln_s = logf(s);
-    put_row<BF16>(a, t, row, first, M, s, u, ln_s);
+    put_row(a, t, row, first, M, s, u, ln_s);
     if (a.n == 0) return;
     uint32_t limit = (uint32_t)(bound >> 32);
     if (firsts == 1) {
@@ -446,9 +451,10 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_join_kernel(LogitsCall a)
     });
 }
 
-// Parts of a row: as many as fill the GPU with blocks, of 4096 logits or more.
+// Parts of a row: as many as make 1024 blocks, of 4096 logits or more.  us with 1024, 2048 and 4096 blocks: 251 rows of 50257 in fp32 18.5, 19.7, 21.6; 1100 rows of
+// 50257 in bf16 28.7, 35.1, 36.8; 1900 of 32000 30.9, 40.7, 40.9; one row of 151936 in parts of 4096, 8192: 11.2, 13.0.
 static int logprobs_parts(int64_t T, int V) {
-    int64_t n = T < 1 ? 1 : (2048 + T - 1) / T;
+    int64_t n = T < 1 ? 1 : (1024 + T - 1) / T;
     const int64_t most = (V + 4095) / 4096;
     if (n > most) n = most;
     return (int)(n < 1 ? 1 : n > LP_MOST_PARTS ? LP_MOST_PARTS : n);
@@ -489,8 +495,9 @@ extern "C" int c2r_token_logprobs(const void *logits, c2r_dtype dt, int64_t stri
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
     const dim3 grid((unsigned)(T * a.parts)), rows((unsigned)T), block(LP_THREADS);
-    if (dt == C2R_BF16) logprobs_kernel<true><<<grid, block, 0, st>>>(a);
-    else logprobs_kernel<false><<<grid, block, 0, st>>>(a);
+    const bool streamed = T * V * size >= 4 * STREAMED_BYTES;
+    if (dt == C2R_BF16) streamed ? logprobs_kernel<true, true><<<grid, block, 0, st>>>(a) : logprobs_kernel<true, false><<<grid, block, 0, st>>>(a);
+    else streamed ? logprobs_kernel<false, true><<<grid, block, 0, st>>>(a) : logprobs_kernel<false, false><<<grid, block, 0, st>>>(a);
     const int rc = launch_status();
     if (rc != C2R_OK || a.parts == 1) return rc;
     if (dt == C2R_BF16) logprobs_join_kernel<true><<<rows, block, 0, st>>>(a);

@@ -37,13 +37,19 @@ __device__ __forceinline__ void load8(const unsigned char *p, float (&v)[8]) {
     }
 }
 
-template <bool BF16>
+// (STREAMED: 8192 rows of 2048 in bf16, with the sum and 8 bits, 151 MB: 26.3 us and 30.2 the other way)
+template <bool STREAMED, class T>
+__device__ __forceinline__ void put(unsigned char *p, const T &v) {
+    if constexpr (STREAMED) __builtin_nontemporal_store(v, reinterpret_cast<T *>(p));
+    else *reinterpret_cast<T *>(p) = v;
+}
+template <bool BF16, bool STREAMED>
 __device__ __forceinline__ void store8(unsigned char *p, const float (&v)[8]) {
     if constexpr (BF16) {
-        *reinterpret_cast<u32x4 *>(p) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+        put<STREAMED>(p, u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])});
     } else {
-        reinterpret_cast<f32x4 *>(p)[0] = f32x4{v[0], v[1], v[2], v[3]};
-        reinterpret_cast<f32x4 *>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
+        put<STREAMED>(p, f32x4{v[0], v[1], v[2], v[3]});
+        put<STREAMED>(p + 16, f32x4{v[4], v[5], v[6], v[7]});
     }
 }
 
@@ -65,7 +71,7 @@ __device__ __forceinline__ float row_total(float v, float *lds) {
 }
 
 // THREADS threads to a row, PIECES pieces of 8 elements to a thread.
-template <bool BF16, int THREADS, int PIECES>
+template <bool BF16, int THREADS, int PIECES, bool STREAMED>
 __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void row_norm_kernel(NormCall a) {
     constexpr int BLOCK = THREADS > 256 ? THREADS : 256, SZ = BF16 ? 2 : 4;
     __shared__ float sums[BLOCK / 64], tops[BLOCK / 64];
@@ -113,12 +119,12 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void row_norm_kernel
     for (int i = 0; i < PIECES; ++i) {
         const int p = i * THREADS + lane;
         if (p >= pieces) continue;
-        if (a.sum) store8<BF16>(a.sum + t * a.sum_bytes + (int64_t)p * (8 * SZ), s[i]);
+        if (a.sum) store8<BF16, STREAMED>(a.sum + t * a.sum_bytes + (int64_t)p * (8 * SZ), s[i]);
         float w[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
         if (a.weight) load8<false>(reinterpret_cast<const unsigned char *>(a.weight + (int64_t)p * 8), w);
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[i][e] = s[i][e] * by * w[e], top = fmaxf(top, fabsf(s[i][e]));
-        if (a.y) store8<BF16>(a.y + t * a.y_bytes + (int64_t)p * (8 * SZ), s[i]);
+        if (a.y) store8<BF16, STREAMED>(a.y + t * a.y_bytes + (int64_t)p * (8 * SZ), s[i]);
     }
     if (!a.y8) return;
     top = row_total<THREADS, true>(top, tops);
@@ -137,14 +143,16 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void row_norm_kernel
             w[e] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2] * inv, v[3] * inv, low, true);
         }
 #endif
-        *reinterpret_cast<u32x2 *>(a.y8 + t * a.y8_bytes + (int64_t)p * 8) = w;
+        put<STREAMED>(a.y8 + t * a.y8_bytes + (int64_t)p * 8, w);
     }
 }
 
 template <bool BF16, int THREADS, int PIECES>
 static void norm(const NormCall &a, hipStream_t st) {
     constexpr int BLOCK = THREADS > 256 ? THREADS : 256, ROWS = BLOCK / THREADS;
-    row_norm_kernel<BF16, THREADS, PIECES><<<dim3((unsigned)((a.T + ROWS - 1) / ROWS)), dim3(BLOCK), 0, st>>>(a);
+    const dim3 grid((unsigned)((a.T + ROWS - 1) / ROWS)), block(BLOCK);
+    if (a.T * a.d * (BF16 ? 2 : 4) >= STREAMED_BYTES) row_norm_kernel<BF16, THREADS, PIECES, true><<<grid, block, 0, st>>>(a);
+    else row_norm_kernel<BF16, THREADS, PIECES, false><<<grid, block, 0, st>>>(a);
 }
 
 template <bool BF16, int THREADS>
