@@ -34,7 +34,7 @@ struct AdapterCall {
     bool in_blocks;     // the first product's blocks work the order out
     bool copy_rest;     // rows without an adapter are copied
     AdapterTile *tiles;
-    int *slots;         // the row in every slot, -1: none
+    int *slots;         // the row in every slot of a tile's rows
     float *h;           // [parts][slots][16 ranks16]
 };
 
@@ -42,7 +42,7 @@ struct AdapterCall {
 
 // One block: counts, tiles and slots of every adapter.
 __global__ __launch_bounds__(1024) void adapter_order_kernel(AdapterCall a) {
-    __shared__ int next[AD_MOST_ADAPTERS + 1], tiles_of[16];
+    __shared__ int next[AD_MOST_ADAPTERS + 1], rows_of[AD_MOST_ADAPTERS], tiles_of[16];
     const int tid = threadIdx.x;
     // a batch of rows' ids is asked for together; the first batch's stay
     constexpr int BATCH = 8;
@@ -66,14 +66,16 @@ __global__ __launch_bounds__(1024) void adapter_order_kernel(AdapterCall a) {
         }
         return atomicAdd(&next[g], 1);
     };
-    for (int t0 = tid; t0 < a.T; t0 += BATCH * 1024) {
-        int ids[BATCH];
-        if (t0 == tid) {
+    // (of one batch the places stay, too: counted from 0 here)
+    int place[BATCH];
 #pragma unroll
-            for (int i = 0; i < BATCH; ++i) ids[i] = held[i];
-        } else {
-            load(t0, ids);
-        }
+    for (int i = 0; i < BATCH; ++i) {
+        held[i] = group(held[i]), place[i] = 0;
+        if (tid + i * 1024 < a.T) place[i] = take(held[i]);
+    }
+    for (int t0 = tid + BATCH * 1024; t0 < a.T; t0 += BATCH * 1024) {
+        int ids[BATCH];
+        load(t0, ids);
 #pragma unroll
         for (int i = 0; i < BATCH; ++i)
             if (t0 + i * 1024 < a.T) take(group(ids[i]));
@@ -88,18 +90,36 @@ __global__ __launch_bounds__(1024) void adapter_order_kernel(AdapterCall a) {
         if (w < tid >> 6) tile += tiles_of[w];
         with_one += tiles_of[w];
     }
-    auto describe = [&](int adapter, int first, int rows, int from, int step) {
-        const int n = (rows + a.tile_rows - 1) / a.tile_rows;
-        for (int i = from; i < n; i += step) a.tiles[first + i] = AdapterTile{adapter, min(rows - i * a.tile_rows, a.tile_rows)};
-        for (int i = rows + from; i < n * a.tile_rows; i += step) a.slots[first * a.tile_rows + i] = -1;
-    };
-    if (tid < a.E) next[tid] = tile * a.tile_rows, describe(tid, tile, mine, 0, 1);
-    describe(-1, with_one, rest, tid, 1024);
-    for (int i = with_one + (rest + a.tile_rows - 1) / a.tile_rows + tid; i < a.max_tiles; i += 1024) a.tiles[i] = AdapterTile{-2, 0};
+    const int rest_tiles = (rest + a.tile_rows - 1) / a.tile_rows;
+    if (tid < a.E) next[tid] = tile * a.tile_rows, rows_of[tid] = mine;
     if (tid == 1023) next[a.E] = with_one * a.tile_rows;  // (E is 1024 at most: no other thread's)
     __syncthreads();
+    for (int i = tid; i < a.max_tiles; i += 1024) {
+        AdapterTile t = {-2, 0};
+        if (i < with_one) {
+            int lo = 0, hi = a.E - 1;  // the last adapter whose slots begin at or before the tile's and that has any rows
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) / 2;
+                if (next[mid] <= i * a.tile_rows) lo = mid;
+                else hi = mid - 1;
+            }
+            t = {lo, min(rows_of[lo] - (i * a.tile_rows - next[lo]), a.tile_rows)};
+        } else if (i < with_one + rest_tiles) {
+            t = {-1, min(rest - (i - with_one) * a.tile_rows, a.tile_rows)};
+        }
+        a.tiles[i] = t;
+    }
+    if (a.T <= BATCH * 1024) {
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int t = tid + i * 1024;
+            if (t < a.T && (held[i] < a.E || a.copy_rest)) a.slots[next[held[i]] + place[i]] = t;
+        }
+        return;
+    }
+    __syncthreads();  // (the tiles have been described: from here on next[] moves)
     for (int t0 = tid; t0 < a.T; t0 += BATCH * 1024) {
-        if (t0 != tid) load(t0, held);
+        load(t0, held);
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
             const int t = t0 + i * 1024, g = group(held[i]);
@@ -300,7 +320,7 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(AdapterCall a) {
         }
     } else {
         tile = a.tiles[slot0 / a.tile_rows];
-        if (threadIdx.x < MG * 16) here[threadIdx.x] = a.slots[slot0 + threadIdx.x];
+        if (threadIdx.x < MG * 16) here[threadIdx.x] = in_tile + (int)threadIdx.x < tile.rows ? a.slots[slot0 + threadIdx.x] : -1;
         __syncthreads();
     }
     const unsigned char *x_row[MG][Strip<X>::LOADS], *a_row[RG][Strip<W>::LOADS];
