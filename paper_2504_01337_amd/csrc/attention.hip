@@ -86,7 +86,8 @@ size_t attention_shared_workspace_bytes(int64_t T, int D, int heads, int kv_head
     if (T <= 0 || D <= 0 || heads <= 0 || kv_heads <= 0) return 0;
     const int64_t rows = T * heads, prefix = (int64_t)ATTN_TILE_BLOCKS * ATTN_TILE_ROWS, cols = heads / kv_heads < 16 ? heads / kv_heads : 16;
     static_assert(ATTN_TILE_BLOCKS * ATTN_TILE_ROWS >= ATTN_DECODE_BLOCKS * 16, "either kernel's parts of a prefix");
-    return round_up((size_t)(prefix + rows + ATTN_DECODE_EVEN_BLOCKS * cols + rows) * (size_t)(D + 2) * 4, 256);
+    // (own keys: parts as in decoding, or two by waves)
+    return round_up((size_t)(prefix + rows + ATTN_DECODE_EVEN_BLOCKS * cols + 2 * rows) * (size_t)(D + 2) * 4, 256);
 }
 
 }  // namespace c2r
@@ -323,6 +324,7 @@ extern "C" int c2r_attention_decode_shared(const void *q, int64_t q_stride, int 
     const int64_t blocks = cache->batch * cache->kv_heads * ceil_div(a.group, 16);
     const int64_t tiles = attn_max_tiles(a, bf16 ? 32 : 16, 1, longest(cache, max_own_len));
     // many sequences with few keys each: a wave for each, of 8 tiles at most
+    static_assert(ATTN_WAVE_MOST <= 2 * ATTN_WAVE_TILES, "two parts at most: the workspace query counts on it");
     a.own_by_wave = blocks >= ATTN_WAVE_SETS && tiles <= ATTN_WAVE_MOST;
     attn_split(a, tiles, a.own_by_wave ? ceil_div(tiles, ATTN_WAVE_TILES) : decode_parts(blocks, tiles));
     if (rows * cache->kv_heads * a.prefix_splits + blocks * a.splits >= ATTN_MOST_BLOCKS) return C2R_ERR_UNSUPPORTED;

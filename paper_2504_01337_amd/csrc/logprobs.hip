@@ -60,11 +60,13 @@ __device__ __forceinline__ float wave_all(float v) {
     return v;
 }
 
-// A lower bound of the n-th largest of 64 lanes' numbers, in their order: its upper half, bit by bit.  Every lane must be active.
+// A lower bound of the n-th largest of 64 lanes' numbers, in their order: its first 16 bits in bf16 (all there are), 24 in fp32, one after another.
+// Every lane must be active.
+template <bool BF16>
 __device__ __forceinline__ uint32_t wave_nth(uint32_t mine, int n) {
     uint32_t at = 0;
 #pragma unroll
-    for (int bit = 31; bit >= 16; --bit) {
+    for (int bit = 31; bit >= (BF16 ? 16 : 8); --bit) {
         const uint32_t next = at | 1u << bit;
         if (__popcll(__ballot(mine >= next)) >= n) at = next;
     }
@@ -281,7 +283,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogitsCall a) {
     if (a.n > 1) {
         const int lane = lane_id();
         const float four = fmaxf(fmaxf(tops[lane], tops[lane + 64]), fmaxf(tops[lane + 128], tops[lane + 192]));
-        const uint32_t at = wave_nth(in_order(four), a.n);
+        const uint32_t at = wave_nth<BF16>(in_order(four), a.n);
         limit = at <= LOWEST ? -__builtin_inff() : from_order(at);
     }
     const bool listed = (p0 + tid < p1 || extra >= 0) && sums.top >= limit;
@@ -432,7 +434,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_join_kernel(LogitsCall a)
     if (a.n == 0) return;
     uint32_t limit = (uint32_t)(bound >> 32);
     if (firsts == 1) {
-        limit = wave_nth(limit, a.n);
+        limit = wave_nth<BF16>(limit, a.n);
     } else {
         if (lane >= a.parts) limit = ~0u;
         for (int w = 32; w; w >>= 1) limit = min(limit, (uint32_t)__shfl_xor((int)limit, w));

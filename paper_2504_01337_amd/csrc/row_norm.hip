@@ -147,12 +147,22 @@ __global__ __launch_bounds__(THREADS > 256 ? THREADS : 256) void row_norm_kernel
     }
 }
 
+// A grid's threads are counted in 32 bits: more rows take several launches.
 template <bool BF16, int THREADS, int PIECES>
-static void norm(const NormCall &a, hipStream_t st) {
+static void norm(NormCall a, hipStream_t st) {
     constexpr int BLOCK = THREADS > 256 ? THREADS : 256, ROWS = BLOCK / THREADS;
-    const dim3 grid((unsigned)((a.T + ROWS - 1) / ROWS)), block(BLOCK);
-    if (a.T * a.d * (BF16 ? 2 : 4) >= STREAMED_BYTES) row_norm_kernel<BF16, THREADS, PIECES, true><<<grid, block, 0, st>>>(a);
-    else row_norm_kernel<BF16, THREADS, PIECES, false><<<grid, block, 0, st>>>(a);
+    constexpr int64_t MOST = ROWS * (1ll << 21);
+    const bool streamed = a.T * a.d * (BF16 ? 2 : 4) >= STREAMED_BYTES;
+    for (int64_t rest = a.T; rest > 0; rest -= MOST) {
+        a.T = rest < MOST ? rest : MOST;
+        const dim3 grid((unsigned)((a.T + ROWS - 1) / ROWS)), block(BLOCK);
+        if (streamed) row_norm_kernel<BF16, THREADS, PIECES, true><<<grid, block, 0, st>>>(a);
+        else row_norm_kernel<BF16, THREADS, PIECES, false><<<grid, block, 0, st>>>(a);
+        auto on = [&](auto *&p, int64_t bytes) {
+            if (p) p += a.T * bytes;
+        };
+        on(a.x, a.x_bytes), on(a.r, a.r_bytes), on(a.sum, a.sum_bytes), on(a.y, a.y_bytes), on(a.y8, a.y8_bytes), on(a.scale, 1);
+    }
 }
 
 template <bool BF16, int THREADS>

@@ -146,6 +146,15 @@ def test_not_finite(c2r, dtype):
     _check(c2r, l[5:], 10)
 
 
+@pytest.mark.parametrize("scale", [1e-6, 1e-3, 0.02])
+def test_logits_close_together(c2r, scale):
+    """Rows whose logits differ in their last bits only, one block's and parts of one."""
+    l = 10 + scale * torch.randn(6, 30000, generator=torch.Generator().manual_seed(7))
+    _check(c2r, l.cuda(), 40)
+    many = l.repeat(200, 1).cuda()
+    assert torch.equal(c2r.token_logprobs(many, None, 40)[2].view(200, 6, 40)[77], c2r.token_logprobs(l.cuda(), None, 40)[2])
+
+
 def test_given_tokens(c2r):
     l = _logits(4, 9, 5000, "f32")
     tokens = torch.tensor([[0, -1, 4999, 5000, 2 ** 31 - 1, 77]] * 9, dtype=torch.int32, device="cuda")

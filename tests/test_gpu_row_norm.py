@@ -100,6 +100,17 @@ def test_rows_around_the_outputs_stay(c2r):
     assert (y8[0] == 0x55).all() and (y8[-1] == 0x55).all() and (y8[:, d:] == 0x55).all() and c[0] == 7 and c[-1] == 7
 
 
+def test_more_rows_than_a_launch_takes(c2r):
+    """2^23 rows are one launch's here; the last rows, and rows around every border, are those of a call of their own."""
+    T, d = 2 * (1 << 23) + 5, 8
+    x = torch.randn((T, d), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").bfloat16()
+    r = x.roll(1, 0)
+    y, s, y8, c = c2r.add_rms_norm(x, r, bits8=True)
+    for lo, hi in ((0, 9), ((1 << 23) - 4, (1 << 23) + 4), ((1 << 24) - 4, T)):
+        ref = c2r.add_rms_norm(x[lo:hi], r[lo:hi], bits8=True)
+        assert all(torch.equal(a[lo:hi].view(torch.uint8), b.view(torch.uint8)) for a, b in zip((y, s, y8, c), ref))
+
+
 def test_zeros_extremes_and_nan(c2r):
     d = 2048
     x = torch.zeros((6, d), device="cuda")

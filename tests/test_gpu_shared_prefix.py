@@ -162,6 +162,36 @@ def test_a_key_that_is_not_finite(c2r, dtype, n, each):
     assert all(sees[:n]) == (each == 1)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("each,group", [(1, 2), (2, 1), (3, 32)])
+def test_many_runs(c2r, dtype, each, group):
+    """More runs than a wave has lanes, some empty, some without a prefix; with 96 rows to each of a key head's they go through LDS in bf16."""
+    n = 70
+    sizes = [0 if i % 9 == 4 else each for i in range(n)]
+    prefix = [0 if i % 7 == 3 else 20 + i for i in range(n)]
+    b = Batch(c2r, dtype, 64, group, 1, 16, sizes, prefix, [1 + i % 40 for i in range(sum(sizes) + 3)], before=2, after=1, seed=each)
+    out = b.run(max_shared_len=89, max_own_len=40)
+    B = len(b.lens)
+    b.check(out, rows=range(0, B, 1 if group < 32 else 11))
+
+
+def test_a_large_batch_of_single_pages(c2r):
+    """131072 rows of results: the workspace that is asked for is enough, and every sequence gets what it gets alone."""
+    B, H, D, page, L = 4096, 32, 64, 64, 40
+    g = torch.Generator(device="cuda").manual_seed(3)
+    k, v = (torch.randn((B + 1, 1, page, D), generator=g, device="cuda").bfloat16() for _ in "kv")
+    k[:, :, :L], v[:, :, :L] = k[:1, :, :L].clone(), v[:1, :, :L].clone()
+    table = torch.arange(B, dtype=torch.int32, device="cuda")[:, None].contiguous()
+    lens = (L + 1 + torch.arange(B, dtype=torch.int32, device="cuda") % (page - L)).contiguous()
+    cache = c2r.PagedKVCache(k, v, table, lens)
+    q = torch.randn((B, H, D), generator=g, device="cuda").bfloat16()
+    i32 = dict(dtype=torch.int32, device="cuda")
+    out = c2r.attention_decode_shared(q, cache, torch.tensor([0, B], **i32), torch.tensor([L], **i32), max_shared_len=L, max_own_len=page - L)
+    ref = c2r.attention_decode(q, cache)
+    # weights rounded to bf16 in the prefix's part, and a result's rounding on either side: 3 * 2^-8 of the largest value
+    assert (out.float() - ref.float()).abs().max() <= 3 * B8 * v.abs().max().float()
+
+
 def test_a_long_prefix_many_sequences(c2r):
     b = Batch(c2r, "bf16", 128, 8, 2, 16, [70], [3000], [1 + 5 * (i % 13) for i in range(70)], seed=1)
     out = b.run(max_shared_len=3000, max_own_len=61)
