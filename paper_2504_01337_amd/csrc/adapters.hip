@@ -4,7 +4,9 @@
 // read once per tile.  Two products on the matrix pipe: h = A_a x (contraction d_in, a block's waves share it out and add up
 // through LDS, blocks share it out where there are few) and B_a h (contraction r), with y added in 32 bits and one rounding.
 // h stays in 32 bits: bf16 takes it in two pieces, the rounded number and what is left of it.
-// Bound by memory: x, y, out and the adapters in use.
+// Bound by memory: x, y, out and the adapters in use.  8192 rows in e4m3, 2048 to 6144, rank 16: 55 us of a call (219 MB: 4.0 TB/s), of which the second
+// product 40, the first 8.5, the order of the rows 7; 131 rows, 4096 to 6144, 20 adapters of rank 64: 15 (30 MB), of which 8.6 and 7; one row 5.5 and
+// 4, a launch and a chain of dependent loads each.
 #include "ffn_copy.h"
 
 namespace c2r {

@@ -2,6 +2,8 @@
 // rows go, and not once for a sequence.  The rows of a block are either (sequence, query head) pairs of one run and one key head, against
 // a part of the run's keys, or the query heads of one sequence that share a key head, against a part of the keys behind.  All
 // results are partial, and joined.  Prefixes in bf16 that many rows look at go through LDS in blocks of 128 rows (attn_tile.h), in the same launch.
+// Bound by memory: 64 sequences behind five prefixes of up to 4000 with up to 2000 keys each, 16 heads 131 us (5.4 TB/s), joined in 5; four behind 2000 9
+// and 4, latency.  131 sequences of 32 / 8 heads behind 8000 keys with up to 500 each: 56 and 6, of which either kind of block alone takes 35.
 #include "attn_stream.h"
 #include "attn_tile.h"
 

@@ -1,7 +1,9 @@
 // The residual's sum and the root-mean-square norm of whole rows, with the rows in bf16 or fp32, in 8 bits with a scale each, or both:
 //     s = x + r (rounded as it is kept),  y = s * rsqrt(mean(s^2) + eps) * weight,  c = max |y| / 448,  y8 = y / c
 // A row is read once: its elements stay in the registers of the lanes that loaded them, 8 at a time, while the two numbers that
-// a whole row has to give (the sum of squares, then the largest |y|) go round.  Bound by memory.
+// a whole row has to give (the sum of squares, then the largest |y|) go round: within a wave up to rows of 4096, and within a block for longer rows or
+// few of them (one row of 2048: 2.4 us with a block, of which 2 are a launch's).  Bound by memory: 8192 rows of 2048 in bf16, with the sum
+// and 8 bits, 24 us (6.2 TB/s; the library's copy reaches 5.05); 517 rows of 256 in fp32 3.0.
 #include "c2r_internal.h"
 
 namespace c2r {
