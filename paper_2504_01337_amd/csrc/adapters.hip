@@ -354,7 +354,7 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(AdapterCall a) {
         for (int i = 0; i < DEPTH; ++i) {
             const int k = (s + 4 * i) * STEP, in = s + 4 * i < s1 ? a.d_in - k : 0;
 #pragma unroll
-            for (int q = 0; q < RG; ++q) as[i][q].load([&](int l) { return a_row[q][l]; }, k, in);
+            for (int q = 0; q < RG; ++q) as[i][q].load([&](int l) { return a_row[q][l]; }, k, chunk * RG + q < a.ranks16 ? in : 0);
 #pragma unroll
             for (int m = 0; m < MG; ++m) xs[i][m].load([&](int l) { return x_row[m][l]; }, k, in);
         }
@@ -548,7 +548,7 @@ static AdapterPlan adapter_plan(int64_t T, int d_in, int E, int r) {
     p.tiles = T / p.tile_rows + groups;
     if (p.tiles > T) p.tiles = T;
     p.down_blocks = p.tiles * (p.tile_rows / p.down_rows) * ((p.ranks16 + p.rank_groups - 1) / p.rank_groups);
-    int64_t parts = (256 + p.down_blocks - 1) / p.down_blocks;
+    int64_t parts = (512 + p.down_blocks - 1) / p.down_blocks;
     const int64_t most = d_in / 512;
     if (parts > most) parts = most;
     p.parts = (int)(parts < 1 ? 1 : parts);

@@ -313,7 +313,13 @@ extern "C" int c2r_attention_decode_shared(const void *q, int64_t q_stride, int 
     // the prefixes
     const bool tiled = bf16 && cache->batch * a.group > ATTN_PREFIX_ROWS * n_shared;
     const int64_t per_block = tiled ? ATTN_TILE_ROWS : 16, KT = tiled ? 64 : bf16 ? 32 : 16;
-    const int64_t rows = cache->batch * a.group / per_block + n_shared, prefix_tiles = ceil_div(longest(cache, max_shared_len), KT);
+    const int64_t rows = cache->batch * a.group / per_block + n_shared;
+    // (of a prefix that lies before a sequence's own keys, a window leaves its own length at most)
+    int64_t prefix_tiles = ceil_div(longest(cache, max_shared_len), KT);
+    if (a.window) {
+        const int64_t near = ceil_div(a.window, KT) + 1 + ceil_div(a.sinks, KT);
+        if (near < prefix_tiles) prefix_tiles = near;
+    }
     int64_t parts = attn_parts(rows * cache->kv_heads, prefix_tiles, tiled ? ATTN_PREFIX_BLOCKS : ATTN_DECODE_BLOCKS, tiled ? ATTN_TILE_TILES : ATTN_DECODE_TILES);
     // (no more blocks than CUs: one too many takes as long as as many again)
     if (tiled && parts > 1 && parts * rows * cache->kv_heads > ATTN_PREFIX_BLOCKS) --parts;

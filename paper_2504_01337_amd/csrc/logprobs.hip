@@ -62,15 +62,18 @@ __device__ __forceinline__ float wave_all(float v) {
     return v;
 }
 
-// A lower bound of the n-th largest of 64 lanes' numbers, in their order: its first 16 bits in bf16 (all there are), 24 in fp32, one after another.
+// A lower bound of the n-th largest of 64 lanes' numbers (EACH of a lane's), in their order: its first 16 bits in bf16 (all there are), 24 in fp32, one after another.
 // Every lane must be active.
-template <bool BF16>
-__device__ __forceinline__ uint32_t wave_nth(uint32_t mine, int n) {
+template <bool BF16, int EACH>
+__device__ __forceinline__ uint32_t wave_nth(const uint32_t (&mine)[EACH], int n) {
     uint32_t at = 0;
 #pragma unroll
     for (int bit = 31; bit >= (BF16 ? 16 : 8); --bit) {
         const uint32_t next = at | 1u << bit;
-        if (__popcll(__ballot(mine >= next)) >= n) at = next;
+        int reach = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) reach += __popcll(__ballot(mine[i] >= next));
+        if (reach >= n) at = next;
     }
     return at;
 }
@@ -280,12 +283,19 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogitsCall a) {
     if (a.n == 0) return;
 
     // ---- the n largest ----
-    // a number that n lanes at least reach: of every four lanes' largest the n-th, rounded down
+    // a number that n logits at least reach: of every four lanes' largest the n-th, which few others reach while n is small beside 64, or of every lane's
+    // (109 rows of 63989 in bf16, 64 alternatives: @@ us, and 52 the other way)
     float limit = M;
     if (a.n > 1) {
         const int lane = lane_id();
-        const float four = fmaxf(fmaxf(tops[lane], tops[lane + 64]), fmaxf(tops[lane + 128], tops[lane + 192]));
-        const uint32_t at = wave_nth<BF16>(in_order(four), a.n);
+        uint32_t at;
+        if (a.n <= 16) {
+            const uint32_t four[1] = {in_order(fmaxf(fmaxf(tops[lane], tops[lane + 64]), fmaxf(tops[lane + 128], tops[lane + 192])))};
+            at = wave_nth<BF16>(four, a.n);
+        } else {
+            const uint32_t each[4] = {in_order(tops[lane]), in_order(tops[lane + 64]), in_order(tops[lane + 128]), in_order(tops[lane + 192])};
+            at = wave_nth<BF16>(each, a.n);
+        }
         limit = at <= LOWEST ? -__builtin_inff() : from_order(at);
     }
     const bool listed = (p0 + tid < p1 || extra >= 0) && sums.top >= limit;
@@ -436,7 +446,8 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_join_kernel(LogitsCall a)
     if (a.n == 0) return;
     uint32_t limit = (uint32_t)(bound >> 32);
     if (firsts == 1) {
-        limit = wave_nth<BF16>(limit, a.n);
+        const uint32_t one[1] = {limit};
+        limit = wave_nth<BF16>(one, a.n);
     } else {
         if (lane >= a.parts) limit = ~0u;
         for (int w = 32; w; w >>= 1) limit = min(limit, (uint32_t)__shfl_xor((int)limit, w));
