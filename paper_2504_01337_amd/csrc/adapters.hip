@@ -298,92 +298,82 @@ __device__ __forceinline__ f32x4 multiply(const u32x4 &a, const u32x4 &b, f32x4 
     return c;
 }
 
-// Blocks: parts of d_in fastest, then 16 RG ranks, then 16 MG rows of a tile.  A wave's step is 256 bytes of every rank's row (128 elements of d_in,
-// 64 in fp32), and its products leave lane (g, n) with ranks 4 g .. of row n.
-template <int X, int MG, int RG>
+// Blocks: parts of d_in fastest, then 16 RG ranks, then 16 rows of a tile.  A wave's step is 256 bytes of every rank's row (128 elements of d_in,
+// 64 in fp32), and its products leave lane (g, n) with ranks 4 g .. of row n.  (32 or 64 rows to a block read the weights less often, and have fewer
+// loads in flight: 8192 rows of rank 64 75 us of a call, 80 and 97; 4096 to 4096 of rank 128 101, 98, 119.)
+template <int X, int RG>
 __global__ __launch_bounds__(256) void adapter_down_kernel(AdapterCall a) {
     constexpr bool BF16 = X != AD_F32;
     constexpr int W = BF16 ? AD_BF16 : AD_F32, WS = BF16 ? 2 : 4, STEP = 256 / WS;
     __shared__ __align__(16) unsigned char strips[4][4096];
-    __shared__ f32x4 sums[MG * RG == 1 ? 5 : 4][MG * RG][64];  // (also few_rows_tile's)
+    __shared__ f32x4 sums[RG == 1 ? 5 : 4][RG][64];  // (also few_rows_tile's)
     static_assert(sizeof(sums) >= (AD_MOST_ADAPTERS + 1 + 8) * 4, "room for few_rows_tile");
+    __shared__ int here[16];  // the rows of these slots
     const int chunks = (a.ranks16 + RG - 1) / RG, part = blockIdx.x % a.parts, id = blockIdx.x / a.parts, chunk = id % chunks, rows_at = id / chunks;
-    const int slot0 = rows_at * (MG * 16), in_tile = slot0 % a.tile_rows;
+    const int slot0 = rows_at * 16, in_tile = slot0 % a.tile_rows;
     const int lane = lane_id(), wave = threadIdx.x >> 6;
-    __shared__ int here[MG * 16];  // the rows of these slots
     AdapterTile tile;
     if (a.in_blocks) {
         int *const lds = reinterpret_cast<int *>(sums);
-        tile = a.T <= AD_FEW_ROWS ? few_rows_tile(a, slot0 / a.tile_rows, in_tile, MG * 16, here, lds)
-                                  : some_rows_tile(a, slot0 / a.tile_rows, in_tile, MG * 16, here, lds);
+        tile = a.T <= AD_FEW_ROWS ? few_rows_tile(a, slot0 / a.tile_rows, in_tile, 16, here, lds) : some_rows_tile(a, slot0 / a.tile_rows, in_tile, 16, here, lds);
         if (part == 0 && chunk == 0) {  // for the second product
-            if (threadIdx.x < MG * 16) a.slots[slot0 + threadIdx.x] = here[threadIdx.x];
+            if (threadIdx.x < 16) a.slots[slot0 + threadIdx.x] = here[threadIdx.x];
             if (threadIdx.x == 0 && in_tile == 0) a.tiles[slot0 / a.tile_rows] = tile;
         }
     } else {
         tile = a.tiles[slot0 / a.tile_rows];
-        if (threadIdx.x < MG * 16) here[threadIdx.x] = in_tile + (int)threadIdx.x < tile.rows ? a.slots[slot0 + threadIdx.x] : -1;
+        if (threadIdx.x < 16) here[threadIdx.x] = in_tile + (int)threadIdx.x < tile.rows ? a.slots[slot0 + threadIdx.x] : -1;
         __syncthreads();
     }
-    const unsigned char *x_row[MG][Strip<X>::LOADS], *a_row[RG][Strip<W>::LOADS];
-#pragma unroll
-    for (int m = 0; m < MG; ++m)
-#pragma unroll
-        for (int i = 0; i < Strip<X>::LOADS; ++i)  // (an empty slot goes along with row 0)
-            x_row[m][i] = a.x + (int64_t)max(here[m * 16 + i * Strip<X>::ROWS + lane / Strip<X>::PER_ROW], 0) * a.x_bytes;
     const int left = tile.rows - in_tile;
     if (tile.adapter < 0 || left <= 0) return;
+    const unsigned char *x_row[Strip<X>::LOADS], *a_row[RG][4];
+#pragma unroll
+    for (int i = 0; i < Strip<X>::LOADS; ++i)  // (an empty slot goes along with row 0)
+        x_row[i] = a.x + (int64_t)max(here[i * Strip<X>::ROWS + lane / Strip<X>::PER_ROW], 0) * a.x_bytes;
 #pragma unroll
     for (int q = 0; q < RG; ++q)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             a_row[q][i] = a.A + ((int64_t)tile.adapter * a.r + min((chunk * RG + q) * 16 + i * 4 + lane / 16, a.r - 1)) * ((int64_t)a.d_in * WS);
-    f32x4 acc[MG][RG];
+    f32x4 acc[RG];
 #pragma unroll
-    for (int m = 0; m < MG; ++m)
-#pragma unroll
-        for (int q = 0; q < RG; ++q) acc[m][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int q = 0; q < RG; ++q) acc[q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     const int steps = (a.d_in + STEP - 1) / STEP, each = (steps + a.parts - 1) / a.parts;
     const int s1 = min((part + 1) * each, steps);
     // (DEPTH steps are asked for together)
-    constexpr int DEPTH = MG * RG == 1 ? 4 : MG * RG <= 4 ? 2 : 1;
+    constexpr int DEPTH = RG == 1 ? 4 : 2;
     for (int s = part * each + wave; s < s1; s += 4 * DEPTH) {
-        Strip<X> xs[DEPTH][MG];
+        Strip<X> xs[DEPTH];
         Strip<W> as[DEPTH][RG];
 #pragma unroll
         for (int i = 0; i < DEPTH; ++i) {
             const int k = (s + 4 * i) * STEP, in = s + 4 * i < s1 ? a.d_in - k : 0;
 #pragma unroll
             for (int q = 0; q < RG; ++q) as[i][q].load([&](int l) { return a_row[q][l]; }, k, chunk * RG + q < a.ranks16 ? in : 0);
-#pragma unroll
-            for (int m = 0; m < MG; ++m) xs[i][m].load([&](int l) { return x_row[m][l]; }, k, in);
+            xs[i].load([&](int l) { return x_row[l]; }, k, in);
         }
 #pragma unroll
         for (int i = 0; i < DEPTH; ++i) {
-            u32x4 av[RG][4];
+            u32x4 xv[4];
+            xs[i].hand_on(strips[wave], xv);
 #pragma unroll
-            for (int q = 0; q < RG; ++q) as[i][q].hand_on(strips[wave], av[q]);
+            for (int q = 0; q < RG; ++q) {
+                u32x4 av[4];
+                as[i][q].hand_on(strips[wave], av);
 #pragma unroll
-            for (int m = 0; m < MG; ++m) {
-                u32x4 xv[4];
-                xs[i][m].hand_on(strips[wave], xv);
-#pragma unroll
-                for (int q = 0; q < RG; ++q)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[m][q] = multiply<BF16>(av[q][j], xv[j], acc[m][q]);
+                for (int j = 0; j < 4; ++j) acc[q] = multiply<BF16>(av[j], xv[j], acc[q]);
             }
         }
     }
 #pragma unroll
-    for (int m = 0; m < MG; ++m)
-#pragma unroll
-        for (int q = 0; q < RG; ++q) sums[wave][m * RG + q][lane] = acc[m][q];
+    for (int q = 0; q < RG; ++q) sums[wave][q][lane] = acc[q];
     __syncthreads();
-    // lane (g, n) of piece (m, q): ranks 4 g .. of 16, row n of 16
-    for (int i = threadIdx.x; i < MG * RG * 64; i += 256) {
-        const int l = i & 63, mq = i >> 6, at = mq / RG * 16 + (l & 15), rank = (chunk * RG + mq % RG) * 16 + (l >> 4) * 4;
+    // lane (g, n) of piece q: ranks 4 g .. of 16, row n of 16
+    for (int i = threadIdx.x; i < RG * 64; i += 256) {
+        const int l = i & 63, q = i >> 6, at = l & 15, rank = (chunk * RG + q) * 16 + (l >> 4) * 4;
         if (at >= left || rank >= a.ranks16 * 16) continue;
-        f32x4 v = sums[0][mq][l] + sums[1][mq][l] + (sums[2][mq][l] + sums[3][mq][l]);
+        f32x4 v = sums[0][q][l] + sums[1][q][l] + (sums[2][q][l] + sums[3][q][l]);
         float by = a.scale ? a.scale[tile.adapter] : 1.0f;
         if (X == AD_E4M3) by *= a.x_scale[here[at]];
         v *= by;
@@ -533,7 +523,7 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterCall a) {
 // ---- sizes ----
 
 struct AdapterPlan {
-    int tile_rows, down_rows, ranks16, rank_groups, parts;
+    int tile_rows, ranks16, rank_groups, parts;
     int64_t tiles, down_blocks, h_bytes, tile_bytes, slot_bytes;
 };
 
@@ -543,11 +533,10 @@ static AdapterPlan adapter_plan(int64_t T, int d_in, int E, int r) {
     p.tile_rows = T >= 48ll * (E + 1) ? 64 : 16;
     p.ranks16 = (r + 15) / 16;
     p.rank_groups = p.ranks16 >= 3 ? 4 : p.ranks16;
-    p.down_rows = p.tile_rows == 64 && p.ranks16 <= 2 ? 16 : p.tile_rows;
     const int64_t groups = T < E + 1 ? T : E + 1;
     p.tiles = T / p.tile_rows + groups;
     if (p.tiles > T) p.tiles = T;
-    p.down_blocks = p.tiles * (p.tile_rows / p.down_rows) * ((p.ranks16 + p.rank_groups - 1) / p.rank_groups);
+    p.down_blocks = p.tiles * (p.tile_rows / 16) * ((p.ranks16 + p.rank_groups - 1) / p.rank_groups);
     int64_t parts = (512 + p.down_blocks - 1) / p.down_blocks;
     const int64_t most = d_in / 512;
     if (parts > most) parts = most;
@@ -564,12 +553,12 @@ size_t adapters_workspace_bytes(int64_t T, int d_in, int E, int r) {
     return (size_t)(p.tile_bytes + p.slot_bytes + p.h_bytes);
 }
 
-template <int X, int MG>
+template <int X>
 static void adapter_down(const AdapterCall &a, const AdapterPlan &p, hipStream_t st) {
     const dim3 grid((unsigned)(p.down_blocks * p.parts)), block(256);
-    if (p.rank_groups == 1) adapter_down_kernel<X, MG, 1><<<grid, block, 0, st>>>(a);
-    else if (p.rank_groups == 2) adapter_down_kernel<X, MG, 2><<<grid, block, 0, st>>>(a);
-    else adapter_down_kernel<X, MG, 4><<<grid, block, 0, st>>>(a);
+    if (p.rank_groups == 1) adapter_down_kernel<X, 1><<<grid, block, 0, st>>>(a);
+    else if (p.rank_groups == 2) adapter_down_kernel<X, 2><<<grid, block, 0, st>>>(a);
+    else adapter_down_kernel<X, 4><<<grid, block, 0, st>>>(a);
 }
 
 template <bool BF16, int MG, bool STREAMED>
@@ -583,8 +572,7 @@ static void adapter_up(const AdapterCall &a, const AdapterPlan &p, hipStream_t s
 
 template <int X>
 static void adapter_products(const AdapterCall &a, const AdapterPlan &p, hipStream_t st) {
-    if (p.down_rows == 64) adapter_down<X, 4>(a, p, st);
-    else adapter_down<X, 1>(a, p, st);
+    adapter_down<X>(a, p, st);
     const bool streamed = (int64_t)a.T * a.d_out * (X == AD_F32 ? 4 : 2) >= STREAMED_BYTES;
     if (p.tile_rows == 64) streamed ? adapter_up<X != AD_F32, 4, true>(a, p, st) : adapter_up<X != AD_F32, 4, false>(a, p, st);
     else streamed ? adapter_up<X != AD_F32, 1, true>(a, p, st) : adapter_up<X != AD_F32, 1, false>(a, p, st);

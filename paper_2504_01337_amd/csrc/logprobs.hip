@@ -284,7 +284,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogitsCall a) {
 
     // ---- the n largest ----
     // a number that n logits at least reach: of every four lanes' largest the n-th, which few others reach while n is small beside 64, or of every lane's
-    // (109 rows of 63989 in bf16, 64 alternatives: @@ us, and 52 the other way)
+    // (109 rows of 63989 in bf16, 64 alternatives: 22.5 us, and 52 the other way)
     float limit = M;
     if (a.n > 1) {
         const int lane = lane_id();
