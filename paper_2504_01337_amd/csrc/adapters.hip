@@ -389,13 +389,13 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(AdapterCall a) {
 // out are touched in whole stretches of a row, 512 bytes by half a wave (45 us), and pass by the caches (38).  STEPS: products that r takes (32 ranks each in bf16, 16 in fp32);
 // B's rows for all of them, y and h are asked for together.
 template <bool BF16, int MG, int STEPS, bool STREAMED>
-__global__ __launch_bounds__(256) void adapter_up_kernel(AdapterCall a) {
+__global__ __launch_bounds__(256, BF16 && STEPS <= 2 ? 5 : 1) void adapter_up_kernel(AdapterCall a) {
     constexpr int SZ = BF16 ? 2 : 4, KS = BF16 ? 32 : 16, E16 = 16 / SZ, PITCH = STEPS * KS + E16;  // (rows four banks apart)
     constexpr int SLOTS = MG * 16, QUADS = STEPS * KS / 4, H = (SLOTS * QUADS + 255) / 256;
     constexpr int LANES = 256 / E16, ROWS = 256 / LANES, PIECES = 16 / ROWS;  // threads to a row; rows at a time, pieces of a thread's of 16 rows
     constexpr int STAGE = 256 + 4;
     __shared__ __align__(16) unsigned char h_lds[(BF16 ? 2 : 1) * SLOTS * PITCH * SZ];
-    __shared__ __align__(16) float stage[MG > 1 ? 2 : 1][16 * STAGE];
+    __shared__ __align__(16) float stage[16 * STAGE];
     const int col_blocks = (a.d_out + 255) / 256, at = blockIdx.x / col_blocks, c0 = blockIdx.x % col_blocks * 256;
     const AdapterTile tile = a.tiles[at];
     const int lane = lane_id(), wave = threadIdx.x >> 6, g = lane >> 4, n = lane & 15;
@@ -494,8 +494,9 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterCall a) {
                 for (int i = 0; i < 4; ++i) acc[i] = multiply<BF16>(b[k][i], left, acc[i]);
             }
         }
-        // (two stages: a wave has read one before it comes to the barrier behind which others write it again)
-        float *const st = stage[MG > 1 ? m & 1 : 0];
+        // (one stage and five blocks on a CU: 8192 rows of rank 64 74 us of a call, two stages and three blocks 78)
+        float *const st = stage;
+        if (m > 0) lds_hand_over();
 #pragma unroll
         for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4 *>(st + n * STAGE + wave * 64 + i * 16 + g * 4) = acc[i];
         lds_hand_over();
