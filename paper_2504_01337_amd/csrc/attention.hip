@@ -320,9 +320,11 @@ extern "C" int c2r_attention_decode_shared(const void *q, int64_t q_stride, int 
         const int64_t near = ceil_div(a.window, KT) + 1 + ceil_div(a.sinks, KT);
         if (near < prefix_tiles) prefix_tiles = near;
     }
-    int64_t parts = attn_parts(rows * cache->kv_heads, prefix_tiles, tiled ? ATTN_PREFIX_BLOCKS : ATTN_DECODE_BLOCKS, tiled ? ATTN_TILE_TILES : ATTN_DECODE_TILES);
-    // (no more blocks than CUs: one too many takes as long as as many again)
-    if (tiled && parts > 1 && parts * rows * cache->kv_heads > ATTN_PREFIX_BLOCKS) --parts;
+    const int most = tiled ? attn_prefix_blocks(D) : ATTN_DECODE_BLOCKS;
+    int64_t parts = attn_parts(rows * cache->kv_heads, prefix_tiles, most, tiled ? ATTN_TILE_TILES : ATTN_DECODE_TILES);
+    // (no more blocks than that: one too many takes as long as as many again)
+    static_assert(attn_prefix_blocks(64) <= ATTN_TILE_BLOCKS && attn_prefix_blocks(128) <= ATTN_TILE_BLOCKS, "the workspace query counts on it");
+    if (tiled && parts > 1 && parts * rows * cache->kv_heads > most) --parts;
     a.prefix_tiles = (int)ceil_div(prefix_tiles, parts);
     a.prefix_splits = (int)ceil_div(prefix_tiles, a.prefix_tiles);
     a.prefix_blocks = (int)rows;

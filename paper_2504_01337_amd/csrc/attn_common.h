@@ -294,9 +294,14 @@ constexpr int ATTN_BY_ROWS = 2;
 // Blocks of a join from which on keys are not cut: nearly all of them would find nothing to do.
 constexpr int64_t ATTN_JOIN_BLOCKS = 1 << 17;
 
-// Rows of a shared prefix, per key head, from which on its keys go through LDS; the blocks of 128 rows that its parts make at most: one to a CU, beside
-// the sequences' own keys.  131 sequences of 32 / 8 heads behind 8000 keys with up to 500 each, in 3, 4, 5, 6, 7 parts: 80, 68, 60, 61, 69 us.
-constexpr int ATTN_PREFIX_ROWS = 32, ATTN_PREFIX_BLOCKS = 256;
+// Rows of a shared prefix, per key head, above which its keys go through LDS.  us in registers and through LDS, by rows: 16 heads of 128 behind 4000
+// keys 12: 16.4 and 17.1, 16: 17.1 and 17.6, 24: 21.5 and 19.1, 64: 30 and 23, 256: 73 and 45; 16 heads of 64 behind 16000 24: 24.7 and 24.1,
+// 64: 40 and 28.
+// The blocks of 128 rows that its parts make at most: one to a CU, beside the sequences' own keys, with heads of 64 two.  131 sequences of 32 / 8
+// heads of 128 behind 8000 keys with up to 500 each, in 3, 4, 5, 6, 7 parts: 80, 68, 60, 61, 69 us; 128 of 16 heads of 64 behind 16000 with 100 each,
+// at most 256 and 512 blocks: 53 and 37.
+constexpr int ATTN_PREFIX_ROWS = 16;
+constexpr int attn_prefix_blocks(int D) { return D == 64 ? 512 : 256; }
 // Own keys by waves (attn_shared.hip): parts of 8 tiles, where no sequence has more than two and there are enough of them.
 constexpr int ATTN_WAVE_TILES = 8, ATTN_WAVE_MOST = 16, ATTN_WAVE_SETS = 768;
 constexpr int64_t ATTN_MOST_RUNS = 1 << 20;

@@ -184,9 +184,10 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void attn_shared_kernel(Attn
 }
 
 // Prefixes whose keys go through LDS, and the sequences' own keys: the first are bound by the matrix pipe, the others by memory, and side by
-// side on a CU they take little more than the longer of the two.  The prefixes' blocks are first, one to a CU.
+// side on a CU they take little more than the longer of the two.  The prefixes' blocks are first, one to a CU (heads of 64: two).  Four blocks to a CU
+// would be 128 registers, which heads of 64 do not fit (136; 7 of them through memory): 16 sequences of 16 heads behind 4000 keys 26 us for 15.7.
 template <int D, bool ALIGNED, bool ANY_SCALE>
-__global__ __launch_bounds__(256, D == 128 ? 2 : 4) void attn_shared_tile_kernel(AttnCall a, uint32_t prefix_grid) {
+__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void attn_shared_tile_kernel(AttnCall a, uint32_t prefix_grid) {
     __shared__ __align__(1024) union {
         TileLds<D> tile;
         SharedLds<D> own;

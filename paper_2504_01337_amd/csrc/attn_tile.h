@@ -271,15 +271,6 @@ __device__ __forceinline__ void attn_tile_block(const AttnCall &a, int64_t id, T
         const int buf = (x - x0) & 1, base = tiles.base(x);
         wait_copies_but<0>();
         lds_barrier();
-        if constexpr (SHARED) {  // (a run's last block can have few rows: waves without one copy, and leave the CU to its other block)
-            if (left <= 0) {
-                if (x + 1 < x1) {
-                    copy(x + 1, buf ^ 1, 0, T::COPIES);
-                    look_up(x + 2 < x1 ? x + 2 : x + 1);
-                }
-                continue;
-            }
-        }
         // (a wave that sees nothing of a tile that others of its block see goes along: every weight comes out as zero)
         const bool whole = tile_whole<KT>(a, base, p_min, p_max, keys);
         f32x16 s[2];
