@@ -107,6 +107,16 @@ def test_prefixes(c2r, dtype, case):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,H,Hkv,each,prefix", [(64, 2, 2, 16, 1500), (64, 2, 2, 17, 1500), (128, 2, 2, 16, 1500), (128, 2, 2, 17, 1500), (128, 7, 1, 3, 700),
+                                                 (64, 1, 1, 130, 4100), (128, 1, 1, 130, 4100)])
+def test_rows_around_the_change_of_kernels(c2r, dtype, D, H, Hkv, each, prefix):
+    """16 and 17 rows of a key head (3 x 7, too), and two blocks of them, behind a prefix long enough for many parts."""
+    b = Batch(c2r, dtype, D, H, Hkv, 48, [each, each], [prefix, prefix - 65], [1 + 5 * i % 83 for i in range(2 * each)], seed=each)
+    b.check(b.run(max_shared_len=prefix, max_own_len=83))
+    b.check(b.run(max_shared_len=prefix, max_own_len=83, window=200, sinks=3), window=200, sinks=3)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("window,sinks", [(1, 0), (40, 0), (200, 3), (64, 600), (5000, 1)])
 @pytest.mark.parametrize("many", [False, True])
 def test_windows(c2r, dtype, window, sinks, many):
