@@ -531,8 +531,7 @@ int c2r_attention_prefill(const void *q, int64_t q_stride, int64_t T, int heads,
  * max_shared_len, max_own_len : host; the longest prefix, and the most keys that a sequence has behind its prefix (0: not known).
  *                  They only steer the split: results hold for any value.
  * ws             : c2r_workspace_bytes(C2R_STAGE_ATTENTION_SHARED, batch, head_dim, heads, kv_heads, 0, dtype) bytes, 256-aligned
- * Everything else as c2r_attention_decode; bf16's weights of a prefix that more than 16 rows of a key head look at are rounded to bf16, as
- * c2r_attention_prefill's are.
+ * Everything else as c2r_attention_decode, the two bf16 pieces of the weights too.
  */
 int c2r_attention_decode_shared(const void *q, int64_t q_stride, int heads, const c2r_kv_cache *cache, const int32_t *shared_start,
                                 const int32_t *shared_len, int64_t n_shared, int64_t max_shared_len, int64_t max_own_len, float scale,

@@ -294,12 +294,13 @@ constexpr int ATTN_BY_ROWS = 2;
 // Blocks of a join from which on keys are not cut: nearly all of them would find nothing to do.
 constexpr int64_t ATTN_JOIN_BLOCKS = 1 << 17;
 
-// Rows of a shared prefix, per key head, above which its keys go through LDS.  us in registers and through LDS, by rows: 16 heads of 128 behind 4000
-// keys 12: 16.4 and 17.1, 16: 17.1 and 17.6, 24: 21.5 and 19.1, 64: 30 and 23, 256: 73 and 45; 16 heads of 64 behind 16000 24: 24.7 and 24.1,
-// 64: 40 and 28.
+// Rows per run and key head, the batch's mean, above which keys of shared prefixes go through LDS (the host does not know how sequences share
+// out over runs, and the sums are alike up to their last bits either way).  us in registers and through LDS, by rows: 16 heads of 128 behind 4000
+// keys 12: 16.6 and 19.1, 16: 17.1 and 19.2, 17: 20.8 and 19.3, 24: 21.5 and 19.8, 64: 30.5 and 23.9, 256: 74 and 46; 16 heads of 64 behind 16000
+// 16: 22.1 and 27.6, 24: 24.8 and 27.8, 40: 30.6 and 28.9, 64: 40 and 31.
 // The blocks of 128 rows that its parts make at most: one to a CU, beside the sequences' own keys, with heads of 64 two.  131 sequences of 32 / 8
-// heads of 128 behind 8000 keys with up to 500 each, in 3, 4, 5, 6, 7 parts: 80, 68, 60, 61, 69 us; 128 of 16 heads of 64 behind 16000 with 100 each,
-// at most 256 and 512 blocks: 53 and 37.
+// heads of 128 behind 8000 keys with up to 500 each, in 3, 4, 5, 6, 7 parts: 89, 74, 66, 63, 73 us; 128 of 16 heads of 64 behind 16000 with 100 each,
+// at most 256 and 512 blocks: 54 and 37.
 constexpr int ATTN_PREFIX_ROWS = 16;
 constexpr int attn_prefix_blocks(int D) { return D == 64 ? 512 : 256; }
 // Own keys by waves (attn_shared.hip): parts of 8 tiles, where no sequence has more than two and there are enough of them.

@@ -276,6 +276,7 @@ __device__ __forceinline__ void attn_tile_block(const AttnCall &a, int64_t id, T
         f32x16 s[2];
         bf16x8 kf[2][KSTEPS];
         u32x4 vf[2][2][DT], w[2][2];  // V and weights of 32 keys: two products of 16 keys
+        u32x4 rest[2][2];             // SHARED: what the weights' rounding leaves
         // (the addresses are worked out where they are used: held over the loop, they would not fit the registers)
         uint32_t ka = keys_at + buf * (2 * T::BYTES), va = values_at + buf * (2 * T::BYTES);
         asm volatile("" : "+v"(ka), "+v"(va));
@@ -288,7 +289,10 @@ __device__ __forceinline__ void attn_tile_block(const AttnCall &a, int64_t id, T
         // (weights stay where they are worked out, among the products beside them)
         auto pin = [&](int u) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) asm volatile("" : "+v"(w[u][k]));
+            for (int k = 0; k < 2; ++k) {
+                asm volatile("" : "+v"(w[u][k]));
+                if constexpr (SHARED) asm volatile("" : "+v"(rest[u][k]));
+            }
         };
         auto mask = [&](int u) {
             // in keys from this lane's first one on; worked out here and nowhere before (few tiles need it)
@@ -311,6 +315,8 @@ __device__ __forceinline__ void attn_tile_block(const AttnCall &a, int64_t id, T
         // instruction): a row that sees one key is its value exactly.  A second product with what the rounding leaves would give the
         // 32-bit weights' result and costs a quarter to a third: 4 x 2048 tokens 85 us and 109, one prompt of 8192 288 and 383, root mean
         // square error 2.2e-3 and 1.6e-3, of which the result's own rounding is 1.6e-3.
+        // SHARED: both pieces, as single tokens have them everywhere else (attn_stream.h), so that what a sequence gets does not hang on
+        // how many others there are.
         auto weigh = [&](int u) {
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
@@ -319,17 +325,25 @@ __device__ __forceinline__ void attn_tile_block(const AttnCall &a, int64_t id, T
                 const uint32_t pair = pack_bf16x2(lo, hi);
                 w[u][e >> 3][(e >> 1) & 3] = pair;
                 l = add_pair(l, pair);
+                if constexpr (SHARED) {
+                    const uint32_t left = pack_bf16x2(lo - __uint_as_float(pair << 16), hi - __uint_as_float(pair & 0xffff0000u));
+                    rest[u][e >> 3][(e >> 1) & 3] = left;
+                    l = add_pair(l, left);
+                }
             }
         };
 #if defined(__HIP_DEVICE_COMPILE__)
         auto score = [&](int u, int k) { s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u][k], q[k], s[u], 0, 0, 0); };
         auto add = [&](int u, int k, int d) {
             o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[u][k][d]), __builtin_bit_cast(bf16x8, w[u][k]), o[d], 0, 0, 0);
+            if constexpr (SHARED)
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[u][k][d]), __builtin_bit_cast(bf16x8, rest[u][k]), o[d], 0, 0, 0);
         };
         // A wave issues in order, and a product holds the matrix pipe for 32 cycles: in between there is time for some eight
         // vector instructions.  So the softmax of the first 32 keys stands among the scores of the second 32, and theirs among
         // the first 32's values; operands are read from LDS half a stretch ahead of their products.
         constexpr int HK = KSTEPS / 2, HV = DT;  // half of 32 keys' products
+        constexpr int EACH = SHARED ? 2 : 1, WEIGH = SHARED ? 48 : 0;  // products of a step of values; what both pieces of the weights take more
 #define STRETCH(N, READS, OTHERS)                                       \
     _Pragma("unroll") for (int i_ = 0; i_ < (N); ++i_) {                \
         __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);               \
@@ -390,8 +404,8 @@ __device__ __forceinline__ void attn_tile_block(const AttnCall &a, int64_t id, T
         for (int d = 0; d < DT; ++d) read_values(0, 0, d);
         weigh(0);
         part = largest(0);
-        STRETCH(HK, 1, 64 / KSTEPS)
-        STRETCH(HK, 2 * HV / HK, 64 / KSTEPS)
+        STRETCH(HK, 1, (64 + WEIGH) / KSTEPS)
+        STRETCH(HK, 2 * HV / HK, (64 + WEIGH) / KSTEPS)
         pin(0);
         asm volatile("" : "+v"(part), "+v"(l));
         __builtin_amdgcn_sched_barrier(0);
@@ -408,7 +422,7 @@ __device__ __forceinline__ void attn_tile_block(const AttnCall &a, int64_t id, T
             else read_values(1, 0, d - DT);
         }
         weigh(1);
-        STRETCH(2 * DT, 2, 56 / (2 * DT))
+        STRETCH(2 * DT * EACH, 2 / EACH, (56 + WEIGH) / (2 * DT * EACH))
         pin(1);
         asm volatile("" : "+v"(l));
         __builtin_amdgcn_sched_barrier(0);
@@ -418,8 +432,8 @@ __device__ __forceinline__ void attn_tile_block(const AttnCall &a, int64_t id, T
             if (d < DT) read_values(1, 1, d);
         }
         top = max_halves(fmaxf(part, largest(1))) * scale;
-        STRETCH(DT, 2, 2)
-        STRETCH(DT, 0, 2)
+        STRETCH(DT * EACH, 2 / EACH, 2 / EACH)
+        STRETCH(DT * EACH, 0, 2 / EACH)
         asm volatile("" : "+v"(top));
         __builtin_amdgcn_sched_barrier(0);
 #undef STRETCH
