@@ -134,9 +134,7 @@ class Decoder:
         if any(self.lengths):
             raise ValueError("a common beginning comes first")
         n, batch = len(x), len(self.lengths)
-        adapter, self.adapter = self.adapter, None
-        y = self.prompt(x, [n] + [0] * (batch - 1))
-        self.adapter = adapter
+        y = self._prompt(x, [n] + [0] * (batch - 1), None)
         table, size = self.caches[0].page_table, self.caches[0].k.shape[2]
         whole, part = n // size, n % size
         table[1:, :whole] = table[0, :whole]
@@ -165,13 +163,17 @@ class Decoder:
 
     def prompt(self, x, lengths):
         """x[sum(lengths), d]: the next lengths[b] rows of each sequence."""
+        return self._prompt(x, lengths, self.adapter)
+
+    def _prompt(self, x, lengths, adapter):
         self._grow(lengths)
         new = torch.tensor(lengths, dtype=torch.int32)
         q_start = torch.zeros(len(lengths) + 1, dtype=torch.int32)
         q_start[1:] = new.cumsum(0)
         q_start, new = q_start.cuda(), new.cuda()
         self.kv_len += new
-        adapter = None if self.adapter is None else torch.repeat_interleave(self.adapter, new, output_size=len(x))
+        if adapter is not None:
+            adapter = torch.repeat_interleave(adapter, new, output_size=len(x))
         for block, cache in zip(self.blocks, self.caches):
             x = block.forward(x, cache, q_start, max(lengths), self.max_len, adapter)
         return x
