@@ -17,6 +17,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int AD_MOST_ADAPTERS = 1024, AD_MOST_RANK = 128;
+constexpr float BF16_MOST = 3.3895313892515355e38f;  // (2 - 2^-7) 2^127
 
 // What x holds: the weights' type, or e4m3 with a scale for every row beside bf16 weights.
 enum { AD_F32 = 0, AD_BF16 = 1, AD_E4M3 = 2 };
@@ -464,8 +465,11 @@ __global__ __launch_bounds__(256, BF16 && STEPS <= 2 ? 5 : 1) void adapter_up_ke
         }
         unsigned char *to = h_lds + (slot * PITCH + k) * SZ;
         if constexpr (BF16) {
-            const u32x2 w = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-            float left[4];
+            // (what is finite stays so: above bf16's largest number the first piece is that one)
+            float near[4], left[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) near[e] = fabsf(v[e]) < __builtin_inff() ? fminf(fmaxf(v[e], -BF16_MOST), BF16_MOST) : v[e];
+            const u32x2 w = {pack_bf16x2(near[0], near[1]), pack_bf16x2(near[2], near[3])};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float d = v[e] - __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
