@@ -7,6 +7,7 @@ PyTorch fallback: if libc2r_hip.so is missing, importing the functions raises.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 import struct
 from typing import Optional
@@ -641,16 +642,16 @@ def token_logprobs(logits, tokens=None, n_top=0, entropy=True, ws=None, out=None
     L, given = lib(), 0
     if tokens is not None:
         assert tokens.dtype is torch.int32 and tokens.is_cuda and tokens.is_contiguous() and tokens.shape[0] == T
-        given = tokens.numel() // T if T else 0
+        given = math.prod(tokens.shape[1:])
     if out is None:
         f32 = torch.float32
-        lp, ent, top, top_lp = out = (logits.new_empty(tokens.shape, dtype=f32) if given else None, logits.new_empty((T,), dtype=f32) if entropy else None,
+        lp, ent, top, top_lp = out = (None if tokens is None else logits.new_empty(tokens.shape, dtype=f32), logits.new_empty((T,), dtype=f32) if entropy else None,
                                       logits.new_empty((T, n_top), dtype=torch.int32) if n_top else None,
                                       logits.new_empty((T, n_top), dtype=f32) if n_top else None)
         at = [0 if t is None else t.data_ptr() for t in out]
     else:
         lp, ent, top, top_lp = out
-        for t, shape, dtype in ((lp, tokens.shape if given else None, torch.float32), (ent, (T,), torch.float32), (top, (T, n_top), torch.int32),
+        for t, shape, dtype in ((lp, None if tokens is None else tokens.shape, torch.float32), (ent, (T,), torch.float32), (top, (T, n_top), torch.int32),
                                 (top_lp, (T, n_top), torch.float32)):
             assert t is None or (t.shape == shape and t.dtype is dtype)
         at = [_addr(t) for t in out]

@@ -491,8 +491,8 @@ extern "C" int c2r_token_logprobs(const void *logits, c2r_dtype dt, int64_t stri
     if (dt != C2R_F32 && dt != C2R_BF16) return C2R_ERR_INVALID_ARG;
     if (T < 0 || V < 1 || n_given < 0 || n_top < 0 || n_top > V) return C2R_ERR_INVALID_ARG;
     if (T >= (1ll << 24) || V > (1 << 24) || n_top > LP_MOST_TOP || n_given > 1024) return C2R_ERR_UNSUPPORTED;
+    if (T == 0) return C2R_OK;  // (arrays of no rows may have no address)
     if (n_given == 0 && n_top == 0 && !entropy) return C2R_ERR_INVALID_ARG;
-    if (T == 0) return C2R_OK;
     const int size = dt == C2R_BF16 ? 2 : 4;
     if (!logits || !aligned(logits, size) || stride < V || stride > (1ll << 40)) return C2R_ERR_INVALID_ARG;
     if (n_given > 0 && (!tokens || !logprob || !aligned(tokens, 4) || !aligned(logprob, 4))) return C2R_ERR_INVALID_ARG;

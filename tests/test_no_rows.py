@@ -1,0 +1,9 @@
+"""Calls of no rows, whose arrays have no address (no GPU: nothing is enqueued)."""
+from test_serving_limits import _logprobs, c2r  # noqa: F401 (the fixture)
+
+
+def test_logprobs(c2r):  # noqa: F811
+    none = dict(T=0, l=None, tokens=None, lp=None, ent=None, top=None, top_lp=None, ws=None, bytes=0)
+    for kw in (dict(), dict(given=0), dict(n=0), dict(given=0, n=0)):
+        assert _logprobs(c2r, **none, **kw) == c2r.OK, kw
+    assert _logprobs(c2r, given=0, n=0, ent=None) == c2r.ERR_INVALID_ARG
