@@ -196,8 +196,8 @@ extern "C" int c2r_add_rms_norm(const void *x, int64_t x_stride, const void *res
     if (dt != C2R_F32 && dt != C2R_BF16) return C2R_ERR_INVALID_ARG;
     if (T < 0 || d < 1 || !(eps >= 0.0f)) return C2R_ERR_INVALID_ARG;
     if (d % 8 != 0 || d > NORM_MOST || T >= (1ll << 30)) return C2R_ERR_UNSUPPORTED;
+    if (T == 0) return C2R_OK;  // (rows that are none may have no address)
     if ((sum && !residual) || !y8 != !scale || (!sum && !y && !y8)) return C2R_ERR_INVALID_ARG;
-    if (T == 0) return C2R_OK;
     const int size = dt == C2R_BF16 ? 2 : 4;
     if (!rows_ok(x, x_stride, d, size) || (residual && !rows_ok(residual, residual_stride, d, size))) return C2R_ERR_INVALID_ARG;
     if ((sum && !rows_ok(sum, sum_stride, d, size)) || (y && !rows_ok(y, y_stride, d, size))) return C2R_ERR_INVALID_ARG;
