@@ -62,8 +62,8 @@ __device__ __forceinline__ float wave_all(float v) {
     return v;
 }
 
-// A lower bound of the n-th largest of 64 lanes' numbers (EACH of a lane's), in their order: its first 16 bits in bf16 (all there are), 24 in fp32, one after another.
-// Every lane must be active.
+// A lower bound of the n-th largest of 64 lanes' numbers (EACH of a lane's), in their order: its first 16 bits in bf16, 24 in fp32, one after another.
+// In bf16 these are all that a number has (behind them stand ones if it is negative), so that is the n-th largest itself.  Every lane must be active.
 template <bool BF16, int EACH>
 __device__ __forceinline__ uint32_t wave_nth(const uint32_t (&mine)[EACH], int n) {
     uint32_t at = 0;
@@ -75,7 +75,19 @@ __device__ __forceinline__ uint32_t wave_nth(const uint32_t (&mine)[EACH], int n
         for (int i = 0; i < EACH; ++i) reach += __popcll(__ballot(mine[i] >= next));
         if (reach >= n) at = next;
     }
-    return at;
+    return BF16 && !(at >> 31) ? at | 0xffffu : at;
+}
+
+// The same, and one of the numbers: many that are equal are then equal to it.
+template <bool BF16, int EACH>
+__device__ __forceinline__ float wave_nth_of(const uint32_t (&mine)[EACH], int n) {
+    const uint32_t at = wave_nth<BF16>(mine, n);
+    if (at <= LOWEST) return -__builtin_inff();
+    if constexpr (BF16) return from_order(at);
+    float least = __builtin_inff();
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) least = mine[i] >= at ? fminf(least, from_order(mine[i])) : least;
+    return -wave_all<true>(-least);
 }
 
 // STREAMED: each logit is wanted once and there are many: they pass by the caches (4096 rows of 128200 in bf16: 171 us, and 194 the other way).
@@ -288,15 +300,13 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogitsCall a) {
     float limit = M;
     if (a.n > 1) {
         const int lane = lane_id();
-        uint32_t at;
         if (a.n <= 16) {
             const uint32_t four[1] = {in_order(fmaxf(fmaxf(tops[lane], tops[lane + 64]), fmaxf(tops[lane + 128], tops[lane + 192])))};
-            at = wave_nth<BF16>(four, a.n);
+            limit = wave_nth_of<BF16>(four, a.n);
         } else {
             const uint32_t each[4] = {in_order(tops[lane]), in_order(tops[lane + 64]), in_order(tops[lane + 128]), in_order(tops[lane + 192])};
-            at = wave_nth<BF16>(each, a.n);
+            limit = wave_nth_of<BF16>(each, a.n);
         }
-        limit = at <= LOWEST ? -__builtin_inff() : from_order(at);
     }
     const bool listed = (p0 + tid < p1 || extra >= 0) && sums.top >= limit;
     const int place = take_place(listed, &counts[0]);
