@@ -37,3 +37,20 @@ def test_infinite_products_stay_infinite(c2r):  # noqa: F811
     c.A.fill_(1.0)
     out = c.run(c2r).double().cpu().numpy()
     assert (out[:2] == h[:2, None]).all() and np.isfinite(out[2]).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "f32"])
+@pytest.mark.parametrize("what", ["nan", "inf"])
+def test_every_row_that_is_not_finite(c2r, kind, what):  # noqa: F811
+    """A row with a NaN or an infinity, or of an adapter with a NaN in every rank, has no finite result; the others keep theirs."""
+    c = Case(kind, 80, 512, 256, 32, 4, [i % 4 for i in range(80)], seed=9)
+    ref = c.run(c2r)
+    if kind == "e4m3":
+        c.x_scale[7], c.x_scale[41] = float(what), float(what)
+    else:
+        c.x[7, 3], c.x[41, 100] = float(what), -float(what)
+    c.A[3, :, 5] = float("nan")
+    out = c.run(c2r)
+    bad = torch.tensor([i in (7, 41) or i % 4 == 3 for i in range(80)])
+    assert torch.equal(out[~bad], ref[~bad])
+    assert not torch.isfinite(out[bad]).any()
