@@ -531,7 +531,8 @@ int c2r_attention_prefill(const void *q, int64_t q_stride, int64_t T, int heads,
  * max_shared_len, max_own_len : host; the longest prefix, and the most keys that a sequence has behind its prefix (0: not known).
  *                  They only steer the split: results hold for any value.
  * ws             : c2r_workspace_bytes(C2R_STAGE_ATTENTION_SHARED, batch, head_dim, heads, kv_heads, 0, dtype) bytes, 256-aligned
- * Everything else as c2r_attention_decode, the two bf16 pieces of the weights too.
+ * Everything else as c2r_attention_decode, the two bf16 pieces of the weights too; its limits are batch * heads and n_shared * kv_heads below
+ * 2^22 (some larger ones pass).
  */
 int c2r_attention_decode_shared(const void *q, int64_t q_stride, int heads, const c2r_kv_cache *cache, const int32_t *shared_start,
                                 const int32_t *shared_len, int64_t n_shared, int64_t max_shared_len, int64_t max_own_len, float scale,
@@ -542,9 +543,10 @@ int c2r_attention_decode_shared(const void *q, int64_t q_stride, int heads, cons
  * Sec. 4.1's models), in one pass:
  *     s[t] = x[t] + residual[t]           rounded to dt (residual null: s = x)
  *     y[t] = s[t] * rsqrt(mean(s[t]^2) + eps) * weight            (weight null: 1), rounded to dt
- *     y8[t] = y[t] / scale[t] in e4m3,  scale[t] = max |y[t]| / 448, at least 2^-126     (y before its rounding)
+ *     y8[t] = y[t] * (1 / scale[t]) in e4m3,  scale[t] = max |y[t]| / 448, at least 2^-126     (y before its rounding)
  * 32-bit arithmetic.  The outputs that are set are written: sum (only with a residual), y, y8 with scale; the results do not
- * depend on which.  A row with an infinity or a NaN has NaNs.
+ * depend on which.  A row with an infinity or a NaN has NaNs.  (Right next to a tie, the product by 1 / scale may round to the other
+ * e4m3 number than the quotient.)
  * x, residual, sum, y : [T, d] of dt, the strides count elements from one row to the next; each output may be an input (same stride)
  * y8     : bytes [T, d], 8-byte aligned rows;  scale : fp32[T];  weight : fp32[d] (16-byte aligned) or NULL
  * Limits (else C2R_ERR_UNSUPPORTED): d a multiple of 8 up to 32768, T below 2^30.  C2R_ERR_INVALID_ARG: rows that are not
@@ -565,9 +567,12 @@ int c2r_add_rms_norm(const void *x, int64_t x_stride, const void *residual, int6
  * adapter : int32[T] in DEVICE memory;  A : [n_adapters, rank, d_in], B : [n_adapters, d_out, rank] of dt
  * scale   : fp32[n_adapters] or NULL (1);  y, out : [T, d_out] of dt; out may be y (same stride), and rows without an
  *           adapter are then not touched
- * ws      : c2r_workspace_bytes(C2R_STAGE_ADAPTERS, T, d_in, n_adapters, rank, 0, dt) bytes, 256-aligned
- * Limits (else C2R_ERR_UNSUPPORTED): d_in, d_out, rank multiples of 8, rank up to 128, n_adapters up to 1024, T below 2^24, d_in and d_out
- * up to 2^20.  C2R_ERR_INVALID_ARG: rows that are not whole 16-byte pieces (x in e4m3: 8), strides shorter than a row.
+ * ws      : c2r_workspace_bytes(C2R_STAGE_ADAPTERS, T, d_in, n_adapters, rank, 0, dt) bytes, 256-aligned, for exactly this T: fewer rows can
+ *           take more, so one buffer for batches of several sizes is as large as the largest of theirs
+ * A row's NaNs and infinities, and those of its adapter, leave its results not finite (a NaN may stand where the formula gives an infinity).
+ * Limits (else C2R_ERR_UNSUPPORTED): d_in, d_out, rank multiples of 8 (others are filled up with zeros by the caller), rank up to 128,
+ * n_adapters up to 1024, T below 2^24, d_in and d_out up to 2^20, (T / 16 + n_adapters + 1) * ceil(d_out / 256) below 2^24 (some larger
+ * ones pass).  C2R_ERR_INVALID_ARG: rows that are not whole 16-byte pieces (x in e4m3: 8), strides shorter than a row.
  */
 int c2r_adapters(const void *x, int64_t x_stride, const float *x_scale, c2r_dtype dt, int64_t T, int d_in, int d_out, const int32_t *adapter,
                  int n_adapters, int rank, const void *A, const void *B, const float *scale, const void *y, int64_t y_stride, void *out,
@@ -584,7 +589,8 @@ int c2r_adapters(const void *x, int64_t x_stride, const float *x_scale, c2r_dtyp
  * number fills gets token -1 and a NaN.
  * logits : [T, V] of dt, `stride` elements from one row to the next, any alignment of whole elements
  * tokens : int32[T, n_given];  logprob : fp32[T, n_given];  entropy : fp32[T];  top_token : int32[T, n_top];  top_logprob : fp32[T, n_top]
- * ws     : c2r_workspace_bytes(C2R_STAGE_LOGPROBS, T, V, 1, n_top, 0, dt) bytes, 256-aligned (0 for many rows)
+ * ws     : c2r_workspace_bytes(C2R_STAGE_LOGPROBS, T, V, 1, n_top, 0, dt) bytes, 256-aligned, for exactly this T: 0 for many rows, and
+ *          2046 * (16 + 8 * n_top), rounded up to 256, for any number of them
  * Limits (else C2R_ERR_UNSUPPORTED): n_top up to 64, n_given up to 1024, V up to 2^24, T below 2^24.  C2R_ERR_INVALID_ARG: n_top > V, nothing wanted,
  * a stride below V.
  */

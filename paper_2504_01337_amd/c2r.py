@@ -608,8 +608,9 @@ def add_rms_norm(x, residual=None, weight=None, eps=1e-6, dense=True, bits8=Fals
 
 def adapters(x, adapter, A, B, y, scale=None, x_scale=None, ws=None, out=None):
     """Low-rank adapters of many requests beside a projection that they share: out[t] = y[t] + scale[a] * B[a] (A[a] x[t]) with
-    a = adapter[t] (int32[T]; outside [0, n): out[t] = y[t]).  A[n, rank, d_in], B[n, d_out, rank]; x[T, d_in] of their type, or in e4m3
-    with x_scale[T] (add_rms_norm's y8 and scale).  out may be y.  Returns out[T, d_out]."""
+    a = adapter[t] (int32[T]; outside [0, n): out[t] = y[t]).  A[n, rank, d_in], B[n, d_out, rank] (ranks, and both widths, are multiples of 8:
+    fill others up with zeros); x[T, d_in] of their type, or in e4m3 with x_scale[T] (add_rms_norm's y8 and scale).  out may be y.  ws: of the
+    size for exactly this T, or larger.  Returns out[T, d_out]."""
     T, d_in = x.shape
     n, r, _ = A.shape
     d_out, dt = B.shape[1], A.dtype

@@ -5,8 +5,8 @@
 // through LDS, blocks share it out where there are few) and B_a h (contraction r), with y added in 32 bits and one rounding.
 // h stays in 32 bits: bf16 takes it in two pieces, the rounded number and what is left of it.
 // Bound by memory: x, y, out and the adapters in use.  8192 rows in e4m3, 2048 to 6144, rank 16: 55 us of a call (219 MB: 4.0 TB/s), of which the second
-// product 40, the first 8.5, the order of the rows 7; 131 rows, 4096 to 6144, 20 adapters of rank 64: 15 (30 MB), of which 8.6 and 7; one row 5.5 and
-// 4, a launch and a chain of dependent loads each.
+// product 40, the first 8.7, the order of the rows 7; 131 rows, 4096 to 6144, 20 adapters of rank 64: 15 (30 MB), of which 8.6 and 7; one row 5.7 and
+// 4, a launch and a chain of dependent loads each.  fp32: 8192 rows 106 us (472 MB: 4.5 TB/s), 131 rows 23.
 #include "ffn_copy.h"
 
 namespace c2r {
@@ -47,7 +47,7 @@ struct AdapterCall {
 __global__ __launch_bounds__(1024) void adapter_order_kernel(AdapterCall a) {
     __shared__ int next[AD_MOST_ADAPTERS + 1], rows_of[AD_MOST_ADAPTERS], tiles_of[16];
     const int tid = threadIdx.x;
-    // a batch of rows' ids is asked for together; the first batch's stay
+    // rows' ids come in batches; the first batch's stay
     constexpr int BATCH = 8;
     int held[BATCH];
     auto load = [&](int t0, int (&ids)[BATCH]) {
@@ -387,8 +387,8 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(AdapterCall a) {
 
 // Blocks: 256 columns, 64 to a wave, then tiles.  The products leave a lane with pieces of 16 rows, and a load or store whose neighbouring lanes
 // are in different rows takes an address at a time (64 cycles; 8192 x 6144 in bf16 51 us), so they go through LDS, 16 rows at a time, and y and
-// out are touched in whole stretches of a row, 512 bytes by half a wave (45 us), and pass by the caches (38).  STEPS: products that r takes (32 ranks each in bf16, 16 in fp32);
-// B's rows for all of them, y and h are asked for together.
+// out are touched in whole stretches of a row, 512 bytes by half a wave (45 us), and pass by the caches (38).  STEPS: products that r takes (32 ranks each in bf16, 16 in fp32),
+// with B's rows for all of them in registers.
 template <bool BF16, int MG, int STEPS, bool STREAMED>
 __global__ __launch_bounds__(256, BF16 && STEPS <= 2 ? 5 : 1) void adapter_up_kernel(AdapterCall a) {
     constexpr int SZ = BF16 ? 2 : 4, KS = BF16 ? 32 : 16, E16 = 16 / SZ, PITCH = STEPS * KS + E16;  // (rows four banks apart)
@@ -535,8 +535,15 @@ struct AdapterPlan {
 static AdapterPlan adapter_plan(int64_t T, int d_in, int E, int r) {
     AdapterPlan p;
     // (the host does not know how rows share out: as evenly as they might)
+    // Tiles of 16 and 64 rows, us of a call, 2048 to 4096 in bf16, rows of any adapter: 8 adapters of rank 64, 216, 432, 864 rows 14.0 and 16.4, 17.2
+    // and 20.9, 20.7 and 22.5; 30 of rank 16, 744, 1488, 2976 rows 16.4 and 20.0, 19.6 and 22.3, 27.6 and 26.0; of rank 64 22.0 and 25.5, 27.3 and 29.8,
+    // 43.0 and 35.9; requests of 100 rows, 6200 rows of 30 of rank 64 64 and 56.  (What 64 rows save in weights pays from some 2000 rows on; below, fewer blocks
+    // cost a fifth of a call at most.)
     p.tile_rows = T >= 48ll * (E + 1) ? 64 : 16;
     p.ranks16 = (r + 15) / 16;
+    // 16, 32 and 64 ranks to a block of the first product, us of a call, 4096 to 4096, 8 adapters: of rank 48, 1, 131, 1000, 8192 rows 10.9, 10.7, 11.8;
+    // 12.9, 11.6, 12.5; 23.7, 24.9, 27.3; 81, 73, 72; of rank 128 12.6, 12.4, 13.5; 16.2, 17.7, 18.4; 38.5, 33.3, 36.7; 139, 109, 105.  (x is read
+    // once per 64 ranks, which many rows want; few would rather have more blocks.)
     p.rank_groups = p.ranks16 >= 3 ? 4 : p.ranks16;
     const int64_t groups = T < E + 1 ? T : E + 1;
     p.tiles = T / p.tile_rows + groups;

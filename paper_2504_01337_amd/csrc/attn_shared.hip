@@ -2,8 +2,8 @@
 // rows go, and not once for a sequence.  The rows of a block are either (sequence, query head) pairs of one run and one key head, against
 // a part of the run's keys, or the query heads of one sequence that share a key head, against a part of the keys behind.  All
 // results are partial, and joined.  Prefixes in bf16 that many rows look at go through LDS in blocks of 128 rows (attn_tile.h), in the same launch.
-// Bound by memory: 64 sequences behind five prefixes of up to 4000 with up to 2000 keys each, 16 heads 131 us (5.4 TB/s), joined in 5; four behind 2000 9
-// and 4, latency.  131 sequences of 32 / 8 heads behind 8000 keys with up to 500 each: 56 and 6, of which either kind of block alone takes 35.
+// Bound by memory: 64 sequences behind five prefixes of up to 4000 with up to 2000 keys each, 16 heads 132 us (5.4 TB/s), joined in 5; four behind 2000 9
+// and 4, latency.  131 sequences of 32 / 8 heads behind 8000 keys with up to 500 each: 56 and 6; the prefix's blocks alone take 47.5, the others 37.
 #include "attn_stream.h"
 #include "attn_tile.h"
 
@@ -185,7 +185,8 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void attn_shared_kernel(Attn
 
 // Prefixes whose keys go through LDS, and the sequences' own keys: the first are bound by the matrix pipe, the others by memory, and side by
 // side on a CU they take little more than the longer of the two.  The prefixes' blocks are first, one to a CU (heads of 64: two).  Four blocks to a CU
-// would be 128 registers, which heads of 64 do not fit (136; 7 of them through memory): 16 sequences of 16 heads behind 4000 keys 26 us for 15.7.
+// would be 128 registers, which heads of 64 do not fit (142; up to 20 of them through memory): 24 sequences of 16 heads behind 4000 keys 17.8 us for
+// 16.8, 128 24.1 for 21.7.
 template <int D, bool ALIGNED, bool ANY_SCALE>
 __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void attn_shared_tile_kernel(AttnCall a, uint32_t prefix_grid) {
     __shared__ __align__(1024) union {

@@ -5,7 +5,7 @@
 // sums want anyway, bound the n-th largest of the row from below: only lanes whose largest is not under the n-th largest of these are
 // looked through again, some n of 256.  Rows are cut into parts where there are few; a second launch joins them.
 // Bound by memory for many rows: 4096 rows of 128200 in bf16 171 us (6.1 TB/s).  251 rows of 50257 in fp32, five alternatives: 14.4 us and 4 for the
-// join (50 MB); one row of 151936 in bf16, twenty: 6.7 and 3.7, latency.
+// join (50 MB); one row of 151936 in bf16, twenty: 7.4 and 3.9, latency.
 #include "c2r_internal.h"
 
 namespace c2r {
@@ -476,7 +476,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_join_kernel(LogitsCall a)
     });
 }
 
-// Parts of a row: as many as make 1024 blocks, of 4096 logits or more.  us with 1024, 2048 and 4096 blocks: 251 rows of 50257 in fp32 18.5, 19.7, 21.6; 1100 rows of
+// Parts of a row: as many as make 1024 blocks, of some 4096 logits at least (of 2049 where V is 4097).  us with 1024, 2048 and 4096 blocks: 251 rows of 50257 in fp32 18.5, 19.7, 21.6; 1100 rows of
 // 50257 in bf16 28.7, 35.1, 36.8; 1900 of 32000 30.9, 40.7, 40.9; one row of 151936 in parts of 4096, 8192: 11.2, 13.0.
 static int logprobs_parts(int64_t T, int V) {
     int64_t n = T < 1 ? 1 : (1024 + T - 1) / T;
